@@ -83,7 +83,11 @@ typedef enum {
   MHFFN_OP_UNFUSED_FORWARD = 2,
   MHFFN_OP_UNFUSED_BACKWARD = 3, /* mhffn_reference_unfused with dY != NULL */
   MHFFN_OP_MODULE_FORWARD = 4,
-  MHFFN_OP_MODULE_BACKWARD = 5
+  MHFFN_OP_MODULE_BACKWARD = 5,
+  MHFFN_OP_MODULE_RESIDUAL_FORWARD = 6,
+  MHFFN_OP_MODULE_RESIDUAL_BACKWARD = 7,
+  MHFFN_OP_LINEAR_FORWARD = 8,
+  MHFFN_OP_LINEAR_BACKWARD = 9
 } mhffn_op;
 
 typedef struct {
@@ -244,6 +248,113 @@ int mhffn_module_backward(const mhffn_desc* desc, const void* X, const void* W_i
                           const void* dO, void* dX, void* dW_in, void* dW_gate, void* dW_up,
                           void* dW_down, void* dW_r, void* dW_out, void* workspace,
                           size_t workspace_bytes, void* hip_stream);
+
+/* ---- Linear layer with its epilogue; dropout -------------------------------------------
+ *
+ * What stands around the module and beside it in a model: projections with bias, the layers
+ * of a dense FFN, the residual branch with its dropout.
+ *
+ *   Z = X W + b;   Y = R + D(act(Z))
+ *   W [d_in][d_out] row-major, applied from the right; b [d_out]; both dense.
+ *   Z [n_rows][d_out] dense.  Bias, residual R and Z are optional (NULL).
+ *   act: none; relu max(z, 0); silu z / (1 + exp(-z)); gelu z Phi(z), Phi the normal
+ *   distribution function.
+ *
+ * D keeps an element and scales it by 65536 / (65536 - T), or makes it 0 whatever it held;
+ * T = 65536 * dropout, rounded to the nearest whole number (dropout = 1: all are 0; T = 0:
+ * nothing is dropped or scaled).  Which elements stay is never stored: element (i, j) of an
+ * array with n columns stays where the 16-bit half j % 8 (low half of each word first) of
+ * the four words of Philox4x32-10 is at least T.  Its key is `seed`, its counter the pair
+ * (i * ceil(n / 8) + j / 8, offset + call), 64 bits each, low words first.  `rng` points to
+ * { seed, offset } in DEVICE memory, 8-byte aligned, read when the kernels run: a program that replays a
+ * captured graph advances the offset between replays, and the backward of a pass is given
+ * what its forward was given.  `call` tells the dropouts of one step apart.  With T = 0 rng
+ * may be NULL.
+ *
+ * n_rows, d_in and d_out take any size (rows from 0, widths from 1 to 2^20), row strides any
+ * that is at least the width; rows that are not 16-byte aligned, and widths that are no
+ * multiple of 32, cost copies of the operands in the workspace.  Arithmetic is fp32 (bf16:
+ * products on the bf16 MFMA); Z and Y are rounded once to the storage type, and the
+ * activation sees the unrounded Z.  The backward of an activation uses the rounded Z it is
+ * given, and dZ is rounded to the storage type once more as an operand of its two products
+ * (not in db).  Sums are added in a fixed order: results are bit-identical from run to run. */
+typedef enum {
+  MHFFN_ACT_NONE = 0,
+  MHFFN_ACT_RELU = 1,
+  MHFFN_ACT_SILU = 2,
+  MHFFN_ACT_GELU = 3
+} mhffn_activation;
+
+typedef struct {
+  int64_t n_rows;     /* tokens                                                        */
+  int32_t d_in;       /* columns of X and rows of W                                    */
+  int32_t d_out;      /* columns of W and Y                                            */
+  int64_t ld_x;       /* row stride of X and dX in elements (>= d_in); 0 => d_in       */
+  int64_t ld_y;       /* row stride of Y and dY (>= d_out); 0 => d_out                 */
+  int64_t ld_r;       /* row stride of the residual (>= d_out); 0 => d_out             */
+  int32_t dtype;      /* mhffn_dtype of every tensor                                   */
+  int32_t activation; /* mhffn_activation                                              */
+  float dropout;      /* probability that an element is dropped, 0 .. 1                */
+  uint64_t call;      /* which dropout of the step this is                             */
+} mhffn_linear_desc;
+
+/* Bytes of scratch of `op` (MHFFN_OP_LINEAR_FORWARD or _BACKWARD); 0 for an invalid
+ * descriptor as well. */
+size_t mhffn_linear_workspace_bytes(const mhffn_linear_desc* desc, int op);
+
+/* Y and, unless NULL, Z, which the backward of an activation needs.  Y may be the residual
+ * itself (same address and row stride); no other output may overlap an input. */
+int mhffn_linear_forward(const mhffn_linear_desc* desc, const void* X, const void* W,
+                         const void* bias, const void* residual, const void* rng, void* Y,
+                         void* Z, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* dZ = D(dY) act'(Z);  dX = dZ W^T;  dW = X^T dZ;  dbias = the column sums of dZ.  Any
+ * gradient may be NULL => not computed.  Z is read unless the activation is none (relu'(0) = 0).  The
+ * gradient of the residual is dY itself. */
+int mhffn_linear_backward(const mhffn_linear_desc* desc, const void* X, const void* W,
+                          const void* Z, const void* dY, const void* rng, void* dX, void* dW,
+                          void* dbias, void* workspace, size_t workspace_bytes,
+                          void* hip_stream);
+
+/* Dropout by itself: Y = R + D(X), element (i, j) of [n_rows][n_cols]; R may be NULL.  Its
+ * backward is the same call on dY without a residual.  Y may be X or R (same address and
+ * row stride).  Needs no scratch. */
+typedef struct {
+  int64_t n_rows;
+  int32_t n_cols;     /* 1 .. 2^20                                                     */
+  int64_t ld_x;       /* row strides of X, Y, R in elements (>= n_cols); 0 => n_cols   */
+  int64_t ld_y;
+  int64_t ld_r;
+  int32_t dtype;      /* mhffn_dtype of X, Y, R                                        */
+  float dropout;
+  uint64_t call;
+} mhffn_dropout_desc;
+int mhffn_dropout(const mhffn_dropout_desc* desc, const void* X, const void* residual,
+                  const void* rng, void* Y, void* hip_stream);
+
+/* The module with the residual branch of the layer around it:
+ *     Q = X W_in;   S = mhffn_forward(Q);   O = R + D(S W_out).
+ * Arguments as for mhffn_module_forward; residual [n_tokens][d_model] with row stride ld_r
+ * (0 => d_model) may be NULL, and may be O or X itself.  dropout, rng and call as for the linear
+ * layer (n_tokens rows, d_model columns).  Scratch: MHFFN_OP_MODULE_RESIDUAL_FORWARD. */
+int mhffn_module_residual_forward(const mhffn_desc* desc, const void* X, const void* W_in,
+                                  const void* W_gate, const void* W_up, const void* W_down,
+                                  const void* W_r, const void* W_out, const void* residual,
+                                  int64_t ld_r, float dropout, const void* rng, uint64_t call,
+                                  void* O, void* Q, void* S, void* workspace,
+                                  size_t workspace_bytes, void* hip_stream);
+
+/* Its backward: mhffn_module_backward on D(dO).  The gradient of the residual is dO itself.
+ * Scratch: MHFFN_OP_MODULE_RESIDUAL_BACKWARD (that of mhffn_module_backward, whose dS and dQ
+ * it begins with, and one [n_tokens][d_model] buffer behind it). */
+int mhffn_module_residual_backward(const mhffn_desc* desc, const void* X, const void* W_in,
+                                   const void* W_gate, const void* W_up, const void* W_down,
+                                   const void* W_r, const void* W_out, const void* Q,
+                                   const void* S, const void* dO, float dropout,
+                                   const void* rng, uint64_t call, void* dX, void* dW_in,
+                                   void* dW_gate, void* dW_up, void* dW_down, void* dW_r,
+                                   void* dW_out, void* workspace, size_t workspace_bytes,
+                                   void* hip_stream);
 
 /* Optional set-up for the calling thread's current device: raises the
  * dynamic-LDS limit of every kernel of the library there, so that no later call

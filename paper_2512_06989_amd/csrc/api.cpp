@@ -6,6 +6,7 @@
 #include "mhffn_device.h"
 #include "mhffn_internal.h"
 
+#include <math.h>
 #include <string.h>
 
 #include <mutex>
@@ -91,6 +92,37 @@ int check_fused_shape(const mhffn_desc* d, const Problem& p, bool backward = fal
   return MHFFN_OK;
 }
 
+// Dropout of an array with rows that exist (`reads`: whether the kernels would read the generator).
+int check_dropout(float p, const void* rng, uint64_t call, bool reads, mhffn::Dropout* d) {
+  if (!(p >= 0.0f && p <= 1.0f)) return MHFFN_ERR_SHAPE;   // also rejects NaN
+  d->threshold = (uint32_t)lrintf(p * 65536.0f);
+  d->scale = d->threshold < 65536 ? 65536.0f / (float)(65536 - d->threshold) : 0.0f;
+  d->call = call;
+  d->rng = static_cast<const uint64_t*>(rng);
+  if (reads && d->threshold != 0 && !rng) return MHFFN_ERR_NULL;
+  return (reinterpret_cast<uintptr_t>(rng) & 7u) ? MHFFN_ERR_ALIGN : MHFFN_OK;
+}
+
+constexpr int64_t kMostRows = (int64_t)1 << 40, kMostWidth = 1 << 20;
+
+int check_linear(const mhffn_linear_desc* d, const void* rng, mhffn::Linear* p) {
+  if (!d) return MHFFN_ERR_NULL;
+  if (d->n_rows < 0 || d->n_rows > kMostRows || d->d_in < 1 || d->d_out < 1 || d->d_in > kMostWidth ||
+      d->d_out > kMostWidth)
+    return MHFFN_ERR_SHAPE;
+  if (d->dtype != MHFFN_F32 && d->dtype != MHFFN_BF16) return MHFFN_ERR_UNSUPPORTED;
+  if (d->activation < MHFFN_ACT_NONE || d->activation > MHFFN_ACT_GELU) return MHFFN_ERR_UNSUPPORTED;
+  if ((d->ld_x != 0 && d->ld_x < d->d_in) || (d->ld_y != 0 && d->ld_y < d->d_out) ||
+      (d->ld_r != 0 && d->ld_r < d->d_out))
+    return MHFFN_ERR_SHAPE;
+  p->M = d->n_rows; p->K = d->d_in; p->N = d->d_out;
+  p->ldx = d->ld_x ? d->ld_x : p->K;
+  p->ldy = d->ld_y ? d->ld_y : p->N;
+  p->ldr = d->ld_r ? d->ld_r : p->N;
+  p->dtype = d->dtype; p->act = d->activation;
+  return check_dropout(d->dropout, rng, d->call, false, &p->drop);
+}
+
 int check_workspace(size_t need, const void* ws, size_t have) {
   if (need == 0) return MHFFN_OK;
   if (!ws || have < need) return MHFFN_ERR_WORKSPACE;
@@ -141,6 +173,12 @@ size_t mhffn_workspace_bytes(const mhffn_desc* desc, int op) {
     case MHFFN_OP_MODULE_BACKWARD:
       if (p.route_mode != MHFFN_ROUTE_PARAMS || check_fused_shape(desc, p, true) != MHFFN_OK) return 0;
       return mhffn::module_workspace_bytes(p, desc->dtype, true);
+    case MHFFN_OP_MODULE_RESIDUAL_FORWARD:
+      if (p.route_mode != MHFFN_ROUTE_PARAMS || check_fused_shape(desc, p) != MHFFN_OK) return 0;
+      return mhffn::module_residual_workspace_bytes(p, desc->dtype, false);
+    case MHFFN_OP_MODULE_RESIDUAL_BACKWARD:
+      if (p.route_mode != MHFFN_ROUTE_PARAMS || check_fused_shape(desc, p, true) != MHFFN_OK) return 0;
+      return mhffn::module_residual_workspace_bytes(p, desc->dtype, true);
     case MHFFN_OP_UNFUSED_FORWARD: return mhffn::unfused_workspace_bytes(p, desc->dtype, false);
     case MHFFN_OP_UNFUSED_BACKWARD: return mhffn::unfused_workspace_bytes(p, desc->dtype, true);
     default: return 0;
@@ -342,6 +380,128 @@ int mhffn_module_backward(const mhffn_desc* desc, const void* X, const void* W_i
   const int e = mhffn::launch_module_backward(p, desc->dtype, X, W_in, W_gate, W_up, W_down, W_r,
                                               W_out, Q, S, dO, dX, dW_in, dW_gate, dW_up, dW_down,
                                               dW_r, dW_out, workspace, hip_stream);
+  if (e == -1) return MHFFN_ERR_UNSUPPORTED;
+  return e == 0 ? MHFFN_OK : MHFFN_ERR_LAUNCH;
+}
+
+size_t mhffn_linear_workspace_bytes(const mhffn_linear_desc* desc, int op) {
+  mhffn::Linear p;
+  if (op != MHFFN_OP_LINEAR_FORWARD && op != MHFFN_OP_LINEAR_BACKWARD) return 0;
+  if (check_linear(desc, nullptr, &p) != MHFFN_OK) return 0;
+  return mhffn::linear_workspace_bytes(p, op == MHFFN_OP_LINEAR_BACKWARD);
+}
+
+int mhffn_linear_forward(const mhffn_linear_desc* desc, const void* X, const void* W, const void* bias,
+                         const void* residual, const void* rng, void* Y, void* Z, void* workspace,
+                         size_t workspace_bytes, void* hip_stream) {
+  mhffn::Linear p;
+  int rc = check_linear(desc, rng, &p);
+  if (rc) return rc;
+  const bool empty = p.M == 0;   // no rows: X, Y may be NULL
+  if (!W || (!empty && (!X || !Y || (p.drop.threshold != 0 && !rng)))) return MHFFN_ERR_NULL;
+  for (const void* q : {X, W, bias, residual, (const void*)Y, (const void*)Z})
+    if (!aligned16(q)) return MHFFN_ERR_ALIGN;
+  rc = check_workspace(mhffn::linear_workspace_bytes(p, false), workspace, workspace_bytes);
+  if (rc) return rc;
+  return mhffn::launch_linear_forward(p, X, W, bias, residual, Y, Z, workspace, hip_stream) == 0 ? MHFFN_OK
+                                                                                                : MHFFN_ERR_LAUNCH;
+}
+
+int mhffn_linear_backward(const mhffn_linear_desc* desc, const void* X, const void* W, const void* Z,
+                          const void* dY, const void* rng, void* dX, void* dW, void* dbias, void* workspace,
+                          size_t workspace_bytes, void* hip_stream) {
+  mhffn::Linear p;
+  int rc = check_linear(desc, rng, &p);
+  if (rc) return rc;
+  const bool empty = p.M == 0;   // no rows: X, Z, dY, dX may be NULL
+  if (!W || (!empty && (!X || !dY || (p.act != MHFFN_ACT_NONE && !Z) || (p.drop.threshold != 0 && !rng))))
+    return MHFFN_ERR_NULL;
+  for (const void* q : {X, W, Z, dY, (const void*)dX, (const void*)dW, (const void*)dbias})
+    if (!aligned16(q)) return MHFFN_ERR_ALIGN;
+  rc = check_workspace(mhffn::linear_workspace_bytes(p, true), workspace, workspace_bytes);
+  if (rc) return rc;
+  return mhffn::launch_linear_backward(p, X, W, Z, dY, dX, dW, dbias, workspace, hip_stream) == 0 ? MHFFN_OK
+                                                                                                 : MHFFN_ERR_LAUNCH;
+}
+
+int mhffn_dropout(const mhffn_dropout_desc* desc, const void* X, const void* residual, const void* rng, void* Y,
+                  void* hip_stream) {
+  if (!desc) return MHFFN_ERR_NULL;
+  const int64_t M = desc->n_rows, N = desc->n_cols;
+  if (M < 0 || M > kMostRows || N < 1 || N > kMostWidth) return MHFFN_ERR_SHAPE;
+  if (desc->dtype != MHFFN_F32 && desc->dtype != MHFFN_BF16) return MHFFN_ERR_UNSUPPORTED;
+  for (int64_t ld : {desc->ld_x, desc->ld_y, desc->ld_r})
+    if (ld != 0 && ld < N) return MHFFN_ERR_SHAPE;
+  mhffn::Epilogue e = {};
+  const int rc = check_dropout(desc->dropout, rng, desc->call, M > 0, &e.drop);
+  if (rc) return rc;
+  if (M > 0 && (!X || !Y)) return MHFFN_ERR_NULL;
+  if (!aligned16(X) || !aligned16(residual) || !aligned16(Y)) return MHFFN_ERR_ALIGN;
+  e.residual = residual;
+  e.Y = Y;
+  e.M = M; e.N = N;
+  e.ldy = desc->ld_y ? desc->ld_y : N;
+  e.ldr = desc->ld_r ? desc->ld_r : N;
+  return mhffn::launch_dropout(desc->dtype, X, desc->ld_x ? desc->ld_x : N, e, hip_stream) == 0 ? MHFFN_OK
+                                                                                              : MHFFN_ERR_LAUNCH;
+}
+
+int mhffn_module_residual_forward(const mhffn_desc* desc, const void* X, const void* W_in, const void* W_gate,
+                                  const void* W_up, const void* W_down, const void* W_r, const void* W_out,
+                                  const void* residual, int64_t ld_r, float dropout, const void* rng,
+                                  uint64_t call, void* O, void* Q, void* S, void* workspace,
+                                  size_t workspace_bytes, void* hip_stream) {
+  Problem p;
+  int rc = check_desc(desc, &p);
+  if (rc) return rc;
+  if (p.route_mode != MHFFN_ROUTE_PARAMS) return MHFFN_ERR_UNSUPPORTED;
+  const int64_t dm = (int64_t)p.H * p.dh;
+  if (dm > kMostWidth || (ld_r != 0 && ld_r < dm)) return MHFFN_ERR_SHAPE;
+  const bool empty = (p.N == 0);
+  mhffn::Residual r = {residual, ld_r ? ld_r : dm, {}};
+  rc = check_dropout(dropout, rng, call, !empty, &r.drop);
+  if (rc) return rc;
+  if (!W_in || !W_gate || !W_up || !W_down || !W_r || !W_out) return MHFFN_ERR_NULL;
+  if (!empty && (!X || !O || !Q || !S)) return MHFFN_ERR_NULL;
+  for (const void* q : {X, W_in, W_gate, W_up, W_down, W_r, W_out, residual, (const void*)O, (const void*)Q, (const void*)S})
+    if (!aligned16(q)) return MHFFN_ERR_ALIGN;
+  rc = check_fused_shape(desc, p);
+  if (rc) return rc;
+  if (empty) return MHFFN_OK;
+  rc = check_workspace(mhffn::module_residual_workspace_bytes(p, desc->dtype, false), workspace, workspace_bytes);
+  if (rc) return rc;
+  return mhffn::launch_module_forward(p, desc->dtype, X, W_in, W_gate, W_up, W_down, W_r, W_out, O, Q, S, workspace,
+                                      workspace_bytes, hip_stream, &r) == 0 ? MHFFN_OK : MHFFN_ERR_LAUNCH;
+}
+
+int mhffn_module_residual_backward(const mhffn_desc* desc, const void* X, const void* W_in, const void* W_gate,
+                                   const void* W_up, const void* W_down, const void* W_r, const void* W_out,
+                                   const void* Q, const void* S, const void* dO, float dropout, const void* rng,
+                                   uint64_t call, void* dX, void* dW_in, void* dW_gate, void* dW_up, void* dW_down,
+                                   void* dW_r, void* dW_out, void* workspace, size_t workspace_bytes,
+                                   void* hip_stream) {
+  Problem p;
+  int rc = check_desc(desc, &p);
+  if (rc) return rc;
+  if (p.route_mode != MHFFN_ROUTE_PARAMS) return MHFFN_ERR_UNSUPPORTED;
+  if ((int64_t)p.H * p.dh > kMostWidth) return MHFFN_ERR_SHAPE;
+  const bool empty = (p.N == 0);
+  mhffn::Residual r = {};
+  rc = check_dropout(dropout, rng, call, !empty, &r.drop);
+  if (rc) return rc;
+  if (!W_in || !W_gate || !W_up || !W_down || !W_r || !W_out) return MHFFN_ERR_NULL;
+  if (!empty && (!X || !Q || !S || !dO)) return MHFFN_ERR_NULL;
+  for (const void* q : {X, W_in, W_gate, W_up, W_down, W_r, W_out, Q, S, dO, (const void*)dX, (const void*)dW_in,
+                        (const void*)dW_gate, (const void*)dW_up, (const void*)dW_down, (const void*)dW_r,
+                        (const void*)dW_out})
+    if (!aligned16(q)) return MHFFN_ERR_ALIGN;
+  rc = check_fused_shape(desc, p, true);
+  if (rc) return rc;
+  rc = check_workspace(mhffn::module_residual_workspace_bytes(p, desc->dtype, true), workspace, workspace_bytes);
+  if (rc) return rc;
+  const int e = mhffn::launch_module_residual_backward(p, desc->dtype, X, W_in, W_gate, W_up, W_down, W_r, W_out, Q, S,
+                                                       dO, r.drop, dX, dW_in, dW_gate, dW_up, dW_down, dW_r, dW_out,
+                                                       workspace, hip_stream);
   if (e == -1) return MHFFN_ERR_UNSUPPORTED;
   return e == 0 ? MHFFN_OK : MHFFN_ERR_LAUNCH;
 }

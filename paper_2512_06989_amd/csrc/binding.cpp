@@ -290,10 +290,63 @@ PyObject* backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// module_forward(X, W_in, W_gate, W_up, W_down, W_r, W_out, eps, out, stream, workspace) -> (O, Q, S)
+// Row tensor [rows, width]: its row stride in elements (the width for fewer than two rows)
+int64_t row_stride(const at::Tensor& t, int64_t n, int64_t width, const at::Tensor& like) {
+  require(t.dim() == 2 && t.size(0) == n && t.size(1) == width && same_kind(t, like));
+  require(n == 0 || width == 1 || t.stride(1) == 1);
+  if (n < 2) return width;
+  require(t.stride(0) >= width);
+  return t.stride(0);
+}
+at::Tensor optional_tensor(PyObject* o) { return o == Py_None ? at::Tensor() : tensor(o); }
+uint64_t unsigned64(PyObject* o) {
+  const unsigned long long v = PyLong_AsUnsignedLongLong(o);
+  require(!(v == (unsigned long long)-1 && PyErr_Occurred()));
+  return v;
+}
+// The generator's state: two int64 on the device of the rest; undefined for None
+at::Tensor generator(PyObject* o, const at::Tensor& x) {
+  const at::Tensor t = optional_tensor(o);
+  if (t.defined()) dense(t, {2}, at::kLong, x.device());
+  return t;
+}
+// (kernels run on the current device's stream)
+void on_current_device(const at::Tensor& x) {
+  require(x.is_cuda() && x.device().index() == c10::hip::current_device());
+}
+int32_t dtype_code(const at::Tensor& x) {
+  require(x.scalar_type() == at::kBFloat16 || x.scalar_type() == at::kFloat);
+  return x.scalar_type() == at::kBFloat16 ? MHFFN_BF16 : MHFFN_F32;
+}
+at::Tensor scratch(size_t need, PyObject* given, PyObject* stream, const at::Tensor& x) {
+  if (given != Py_None) return tensor(given);
+  if (need == 0) return at::Tensor();
+  std::optional<OnStream> guard;
+  if (stream != Py_None && x.is_cuda()) guard.emplace(stream_of(stream), x);
+  return at::empty({(int64_t)need}, x.options().dtype(at::kByte));
+}
+size_t size_of(const at::Tensor& t) { return t.defined() ? (size_t)t.numel() * t.element_size() : 0; }
+
+// The residual branch around the module: none where neither a residual nor a dropout is given
+struct Branch {
+  bool any;
+  at::Tensor residual, rng;
+  int64_t ld = 0;
+  float p;
+  uint64_t call;
+  Branch(PyObject* rows_, PyObject* p_, PyObject* rng_, PyObject* call_, const at::Tensor& x)
+      : residual(optional_tensor(rows_)), rng(generator(rng_, x)), p((float)number(p_)), call(unsigned64(call_)) {
+    any = residual.defined() || p != 0.0f;
+    if (residual.defined()) ld = row_stride(residual, x.size(0), x.size(1), x);
+    if (any) on_current_device(x);
+  }
+};
+
+// module_forward(X, W_in, W_gate, W_up, W_down, W_r, W_out, eps, out, stream, workspace, residual, p, rng, call)
+//   -> (O, Q, S)
 PyObject* module_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    require(n == 11);
+    require(n == 15);
     Problem p(a[0], a[2], a[3], a[4], a[5], number(a[7]), MHFFN_ROUTE_PARAMS);
     const int64_t N = p.x.size(0), dm = p.x.size(1);
     const at::Tensor w_in = tensor(a[1]), w_out = tensor(a[6]);
@@ -307,23 +360,27 @@ PyObject* module_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
       if (i > 0) dense(t[i], {N, dm}, p.x.scalar_type(), p.x.device());
     }
     p.d.ld_y = rows(t[0], p.x);
-    const Workspace ws(p, MHFFN_OP_MODULE_FORWARD, a[10], a[9]);
+    const Branch r(a[11], a[12], a[13], a[14], p.x);
+    const Workspace ws(p, r.any ? MHFFN_OP_MODULE_RESIDUAL_FORWARD : MHFFN_OP_MODULE_FORWARD, a[10], a[9]);
     void* const stream = stream_of(a[9]);
-    const int rc = unlocked(mhffn_module_forward, &p.d, data(p.x), data(w_in), data(p.wg), data(p.wu),
-                            data(p.wd), data(p.route), data(w_out), data(t[0]), data(t[1]), data(t[2]),
-                            ws.ptr(), ws.bytes, stream);
+    const int rc = r.any ? unlocked(mhffn_module_residual_forward, &p.d, data(p.x), data(w_in), data(p.wg), data(p.wu),
+                                    data(p.wd), data(p.route), data(w_out), data(r.residual), r.ld, r.p, data(r.rng),
+                                    r.call, data(t[0]), data(t[1]), data(t[2]), ws.ptr(), ws.bytes, stream)
+                         : unlocked(mhffn_module_forward, &p.d, data(p.x), data(w_in), data(p.wg), data(p.wu),
+                                    data(p.wd), data(p.route), data(w_out), data(t[0]), data(t[1]), data(t[2]),
+                                    ws.ptr(), ws.bytes, stream);
     if (rc) return status(rc);
-    PyObject* r = PyTuple_New(3);
-    if (!r) return nullptr;
-    for (int i = 0; i < 3; ++i) PyTuple_SET_ITEM(r, i, THPVariable_Wrap(t[i]));
-    return r;
+    PyObject* all = PyTuple_New(3);
+    if (!all) return nullptr;
+    for (int i = 0; i < 3; ++i) PyTuple_SET_ITEM(all, i, THPVariable_Wrap(t[i]));
+    return all;
   });
 }
 
-// module_backward(X, W_in, W_gate, W_up, W_down, W_r, W_out, Q, S, dO, eps, want, out, stream, workspace)
+// module_backward(X, W_in, W_gate, W_up, W_down, W_r, W_out, Q, S, dO, eps, want, out, stream, workspace, p, rng, call)
 PyObject* module_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    require(n == 15);
+    require(n == 18);
     Problem p(a[0], a[2], a[3], a[4], a[5], number(a[10]), MHFFN_ROUTE_PARAMS);
     const int64_t N = p.x.size(0), dm = p.x.size(1);
     const at::Tensor w_in = tensor(a[1]), w_out = tensor(a[6]), q = tensor(a[7]), s = tensor(a[8]), d_o = tensor(a[9]);
@@ -335,9 +392,14 @@ PyObject* module_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
                            {"dW_down", &p.wd}, {"dW_r", &p.route}, {"dW_out", &w_out}};
     at::Tensor t[7];
     gradients(p, a[11], out, grads, t);
-    const Workspace ws(p, MHFFN_OP_MODULE_BACKWARD, a[14], a[13]);
+    const Branch r(Py_None, a[15], a[16], a[17], p.x);
+    const Workspace ws(p, r.any ? MHFFN_OP_MODULE_RESIDUAL_BACKWARD : MHFFN_OP_MODULE_BACKWARD, a[14], a[13]);
     void* const stream = stream_of(a[13]);
-    const int rc = unlocked(mhffn_module_backward, &p.d, data(p.x), data(w_in), data(p.wg), data(p.wu),
+    const int rc = r.any ? unlocked(mhffn_module_residual_backward, &p.d, data(p.x), data(w_in), data(p.wg), data(p.wu),
+                                    data(p.wd), data(p.route), data(w_out), data(q), data(s), data(d_o), r.p,
+                                    data(r.rng), r.call, data(t[0]), data(t[1]), data(t[2]), data(t[3]), data(t[4]),
+                                    data(t[5]), data(t[6]), ws.ptr(), ws.bytes, stream)
+                         : unlocked(mhffn_module_backward, &p.d, data(p.x), data(w_in), data(p.wg), data(p.wu),
                             data(p.wd), data(p.route), data(w_out), data(q), data(s), data(d_o), data(t[0]),
                             data(t[1]), data(t[2]), data(t[3]), data(t[4]), data(t[5]), data(t[6]), ws.ptr(),
                             ws.bytes, stream);
@@ -345,9 +407,130 @@ PyObject* module_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- linear layer, dropout -------------------------------------------------------------------
+struct LinearCall {
+  at::Tensor x, w, rng;
+  mhffn_linear_desc d;
+  LinearCall(PyObject* X, PyObject* W, PyObject* act, PyObject* p, PyObject* rng_, PyObject* call)
+      : x(tensor(X)), w(tensor(W)) {
+    require(x.dim() == 2 && w.dim() == 2 && w.size(0) == x.size(1));
+    d.n_rows = x.size(0);
+    require(w.size(0) <= INT32_MAX && w.size(1) <= INT32_MAX);
+    d.d_in = (int32_t)w.size(0);
+    d.d_out = (int32_t)w.size(1);
+    d.dtype = dtype_code(x);
+    dense(w, w.sizes(), x.scalar_type(), x.device());
+    d.ld_x = row_stride(x, d.n_rows, d.d_in, x);
+    d.ld_y = d.ld_r = d.d_out;
+    d.activation = (int32_t)integer(act);
+    d.dropout = (float)number(p);
+    d.call = unsigned64(call);
+    rng = generator(rng_, x);
+  }
+};
+
+// linear_forward(X, W, bias, residual, act, p, rng, call, save, out, stream, workspace) -> Y or (Y, Z)
+PyObject* linear_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    require(n == 12);
+    LinearCall c(a[0], a[1], a[4], a[5], a[6], a[7]);
+    const int64_t M = c.d.n_rows, N = c.d.d_out;
+    const at::Tensor bias = optional_tensor(a[2]), residual = optional_tensor(a[3]);
+    if (bias.defined()) dense(bias, {N}, c.x.scalar_type(), c.x.device());
+    if (residual.defined()) c.d.ld_r = row_stride(residual, M, N, c.x);
+    at::Tensor y, z;
+    if (a[9] != Py_None) {
+      const Outputs given(a[9]);
+      y = given.get("Y");
+      z = given.get("Z");
+    }
+    const int save = PyObject_IsTrue(a[8]);
+    require(save >= 0);
+    if (!y.defined()) y = at::empty({M, N}, c.x.options());
+    if (!z.defined() && save) z = at::empty({M, N}, c.x.options());
+    c.d.ld_y = row_stride(y, M, N, c.x);
+    if (z.defined()) dense(z, {M, N}, c.x.scalar_type(), c.x.device());
+    on_current_device(c.x);
+    const at::Tensor ws = scratch(mhffn_linear_workspace_bytes(&c.d, MHFFN_OP_LINEAR_FORWARD), a[11], a[10], c.x);
+    void* const stream = stream_of(a[10]);
+    const int rc = unlocked(mhffn_linear_forward, &c.d, data(c.x), data(c.w), data(bias), data(residual), data(c.rng),
+                            data(y), data(z), data(ws), size_of(ws), stream);
+    if (rc) return status(rc);
+    if (!save) return THPVariable_Wrap(y);
+    PyObject* r = PyTuple_New(2);
+    if (!r) return nullptr;
+    PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(y));
+    PyTuple_SET_ITEM(r, 1, THPVariable_Wrap(z));
+    return r;
+  });
+}
+
+// linear_backward(X, W, dY, Z, act, p, rng, call, want, out, stream, workspace) -> gradients
+PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    require(n == 12);
+    LinearCall c(a[0], a[1], a[4], a[5], a[6], a[7]);
+    const int64_t M = c.d.n_rows, N = c.d.d_out;
+    const at::Tensor dy = tensor(a[2]), z = optional_tensor(a[3]);
+    c.d.ld_y = row_stride(dy, M, N, c.x);
+    if (z.defined()) dense(z, {M, N}, c.x.scalar_type(), c.x.device());
+    Outputs out(a[9]);
+    const char* const keys[3] = {"dX", "dW", "dbias"};
+    at::Tensor t[3];
+    require(PyTuple_Check(a[8]));
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(a[8]); ++i) {
+      PyObject* k = PyTuple_GET_ITEM(a[8], i);
+      int j = 0;
+      while (j < 3 && !(PyUnicode_Check(k) && PyUnicode_CompareWithASCIIString(k, keys[j]) == 0)) ++j;
+      require(j < 3);
+      if (out.has(keys[j])) continue;
+      // (dX has X's row stride: the kernels index both with ld_x)
+      out.set(keys[j], j == 0   ? (M < 2 || c.x.is_contiguous() ? at::empty({M, (int64_t)c.d.d_in}, c.x.options())
+                                                                : at::empty_strided(c.x.sizes(), {c.d.ld_x, 1}, c.x.options()))
+                       : j == 1 ? at::empty(c.w.sizes(), c.w.options())
+                                : at::empty({N}, c.w.options()));
+    }
+    for (int j = 0; j < 3; ++j) t[j] = out.get(keys[j]);
+    if (t[0].defined()) require(row_stride(t[0], M, c.d.d_in, c.x) == c.d.ld_x);
+    if (t[1].defined()) dense(t[1], c.w.sizes(), c.x.scalar_type(), c.x.device());
+    if (t[2].defined()) dense(t[2], {N}, c.x.scalar_type(), c.x.device());
+    on_current_device(c.x);
+    const at::Tensor ws = scratch(mhffn_linear_workspace_bytes(&c.d, MHFFN_OP_LINEAR_BACKWARD), a[11], a[10], c.x);
+    void* const stream = stream_of(a[10]);
+    const int rc = unlocked(mhffn_linear_backward, &c.d, data(c.x), data(c.w), data(z), data(dy), data(c.rng), data(t[0]),
+                            data(t[1]), data(t[2]), data(ws), size_of(ws), stream);
+    return rc ? status(rc) : out.release();
+  });
+}
+
+// dropout(X, p, rng, call, residual, out, stream) -> Y
+PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    require(n == 7);
+    const at::Tensor x = tensor(a[0]), residual = optional_tensor(a[4]);
+    require(x.dim() == 2 && x.size(1) <= INT32_MAX);
+    mhffn_dropout_desc d;
+    d.n_rows = x.size(0);
+    d.n_cols = (int32_t)x.size(1);
+    d.dtype = dtype_code(x);
+    d.dropout = (float)number(a[1]);
+    d.call = unsigned64(a[3]);
+    const at::Tensor rng = generator(a[2], x);
+    const at::Tensor y = a[5] == Py_None ? at::empty(x.sizes(), x.options()) : tensor(a[5]);
+    d.ld_x = row_stride(x, d.n_rows, d.n_cols, x);
+    d.ld_y = row_stride(y, d.n_rows, d.n_cols, x);
+    d.ld_r = residual.defined() ? row_stride(residual, d.n_rows, d.n_cols, x) : d.n_cols;
+    on_current_device(x);
+    void* const stream = stream_of(a[6]);
+    const int rc = unlocked(mhffn_dropout, &d, data(x), data(residual), data(rng), data(y), stream);
+    return rc ? status(rc) : THPVariable_Wrap(y);
+  });
+}
+
 #define MHFFN_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {MHFFN_METHOD(forward), MHFFN_METHOD(forward_static), MHFFN_METHOD(backward),
-                         MHFFN_METHOD(module_forward), MHFFN_METHOD(module_backward), {nullptr, nullptr, 0, nullptr}};
+                         MHFFN_METHOD(module_forward), MHFFN_METHOD(module_backward), MHFFN_METHOD(linear_forward),
+                         MHFFN_METHOD(linear_backward), MHFFN_METHOD(dropout), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", "Argument marshalling of the mhffn binding.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,189 @@
+// What follows a matrix product in a linear layer, element by element, and the generator of its
+// dropout:
+//   z = x W + b;   y = r + D(act(z));   D(v) = v * scale where the element stays, 0 elsewhere.
+// Everything works on pieces of eight neighbouring columns of one row (columns 8 c .. 8 c + 7):
+// 16 bytes of bf16, and exactly what one call of the generator decides.
+//
+// The generator is Philox4x32-10 (Salmon, Moraes, Dror, Shaw: "Parallel random numbers: as easy as
+// 1, 2, 3", 2011): ten rounds of two 32 x 32 -> 64 products over a counter of 128 bits.  Key = the
+// seed; counter = (piece, offset + call), both 64 bits, low word first; piece = row * ceil(n / 8) + c.
+// Column 8 c + j stays where half j of the four words (16 bits, low half first) reaches the
+// threshold rint(65536 p).  So an element's fate depends on the seed, the offset and its place
+// alone: whoever needs the mask again computes it again, in any tiling, and it is never stored.
+#pragma once
+
+#include "mhffn_device.h"
+#include "mhffn_internal.h"
+
+namespace mhffn {
+
+// ---- dropout ----------------------------------------------------------------------------------
+struct DropKey { uint32_t k0, k1, c2, c3; };
+
+// (read on the device: a captured graph draws new numbers when the caller advances the offset)
+__device__ __forceinline__ DropKey drop_key(const Dropout& d) {
+  DropKey k = {0, 0, 0, 0};
+  if (d.threshold == 0 || d.threshold > 65535) return k;
+  const uint64_t seed = d.rng[0], step = d.rng[1] + d.call;
+  k.k0 = (uint32_t)seed; k.k1 = (uint32_t)(seed >> 32);
+  k.c2 = (uint32_t)step; k.c3 = (uint32_t)(step >> 32);
+  return k;
+}
+
+__device__ __forceinline__ u32x4 philox4x32_10(uint64_t piece, const DropKey& key) {
+  uint32_t c0 = (uint32_t)piece, c1 = (uint32_t)(piece >> 32), c2 = key.c2, c3 = key.c3, k0 = key.k0, k1 = key.k1;
+#pragma unroll
+  for (int i = 0; i < 10; ++i) {
+    const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
+    c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
+    c1 = (uint32_t)p1;
+    c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
+    c3 = (uint32_t)p0;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return u32x4{c0, c1, c2, c3};
+}
+
+// A dropped element is 0 whatever it held, infinities and NaN among it.
+__device__ __forceinline__ void drop8(float (&v)[8], uint64_t piece, const Dropout& d, const DropKey& key) {
+  if (d.threshold == 0) return;
+  if (d.threshold > 65535) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    return;
+  }
+  const u32x4 w = philox4x32_10(piece, key);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t half = j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xFFFFu;
+    v[j] = half >= d.threshold ? v[j] * d.scale : 0.f;
+  }
+}
+
+// ---- activations (ACT: mhffn_activation) --------------------------------------------------------
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+  if constexpr (ACT == 1) return z < 0.f ? 0.f : z;              // (NaN stays NaN)
+  else if constexpr (ACT == 2) return z * sigmoid_fast(z);
+  else if constexpr (ACT == 3) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+  else return z;
+}
+// act'(z)
+template <int ACT>
+__device__ __forceinline__ float slope(float z) {
+  if constexpr (ACT == 1) return z <= 0.f ? 0.f : 1.f;
+  else if constexpr (ACT == 2) {
+    const float s = sigmoid_fast(z);
+    return s + z * s * (1.f - s);
+  } else if constexpr (ACT == 3) {
+    return 0.5f * (1.f + erff(z * 0.70710678118654752f)) +
+           z * (0.39894228040143268f * __builtin_amdgcn_exp2f(-0.5f * MHFFN_LOG2E * z * z));
+  } else return 1.f;
+}
+template <int ACT>
+__device__ __forceinline__ void activate8(float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = activate<ACT>(v[j]);
+}
+__device__ __forceinline__ void activate8(float (&v)[8], int act) {
+  if (act == 1) activate8<1>(v);
+  else if (act == 2) activate8<2>(v);
+  else if (act == 3) activate8<3>(v);
+}
+template <int ACT>
+__device__ __forceinline__ void slope8(float (&v)[8], const float (&z)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] *= slope<ACT>(z[j]);
+}
+__device__ __forceinline__ void slope8(float (&v)[8], const float (&z)[8], int act) {
+  if (act == 1) slope8<1>(v, z);
+  else if (act == 2) slope8<2>(v, z);
+  else if (act == 3) slope8<3>(v, z);
+}
+
+// ---- pieces of eight columns in memory -----------------------------------------------------------
+// `cols`: how many of the eight exist; `vec`: rows are 16-byte aligned (a whole piece moves at once).
+__device__ __forceinline__ void unpack8(u32x4 w, float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[2 * j] = __builtin_bit_cast(float, w[j] << 16);
+    v[2 * j + 1] = __builtin_bit_cast(float, w[j] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void load8(const uint16_t* p, int cols, bool vec, float (&v)[8]) {
+  if (vec && cols >= 8) {
+    unpack8(*reinterpret_cast<const u32x4*>(p), v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < cols ? bf16_bits_to_f32(p[j]) : 0.f;
+  }
+}
+__device__ __forceinline__ void load8(const float* p, int cols, bool vec, float (&v)[8]) {
+  if (vec && cols >= 8) {
+    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { v[j] = a[j]; v[4 + j] = b[j]; }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < cols ? p[j] : 0.f;
+  }
+}
+__device__ __forceinline__ void store8(uint16_t* p, int cols, bool vec, const float (&v)[8]) {
+  const u32x4 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+  if (vec && cols >= 8) {
+    *reinterpret_cast<u32x4*>(p) = w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < cols) p[j] = (uint16_t)(j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xFFFFu);
+  }
+}
+__device__ __forceinline__ void store8(float* p, int cols, bool vec, const float (&v)[8]) {
+  if (vec && cols >= 8) {
+    reinterpret_cast<f32x4*>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
+    reinterpret_cast<f32x4*>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < cols) p[j] = v[j];
+  }
+}
+
+// ---- the epilogue of one piece ---------------------------------------------------------------------
+// v: the product's eight sums in, what was stored in Y out.  The residual is read before Y is
+// written, by the same thread: Y may be the residual itself.
+template <typename T>
+__device__ __forceinline__ void epilogue8(float (&v)[8], int64_t row, int64_t col, const Epilogue& e, const DropKey& key) {
+  const int cols = (int)(e.N - col < 8 ? e.N - col : 8);
+  if (e.bias) {
+    float b[8];
+    load8(static_cast<const T*>(e.bias) + col, cols, true, b);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += b[j];
+  }
+  if (e.Z) store8(static_cast<T*>(e.Z) + row * e.ldz + col, cols, e.vec & 1, v);
+  activate8(v, e.act);
+  drop8(v, (uint64_t)row * (uint64_t)((e.N + 7) >> 3) + (uint64_t)(col >> 3), e.drop, key);
+  if (e.residual) {
+    float r[8];
+    load8(static_cast<const T*>(e.residual) + row * e.ldr + col, cols, e.vec & 2, r);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += r[j];
+  }
+  store8(static_cast<T*>(e.Y) + row * e.ldy + col, cols, e.vec & 4, v);
+}
+
+// ---- division by a number that the host knows ----------------------------------------------------------
+// x / d for x < 2^32: m = ceil(2^64 / d) (d > 1), the product's upper 64 bits
+struct Divisor { uint32_t d, m_hi, m_lo; };
+inline Divisor make_divisor(uint32_t d) {
+  const uint64_t m = d > 1 ? ~(uint64_t)0 / d + 1 : 0;
+  return {d, (uint32_t)(m >> 32), (uint32_t)m};
+}
+__device__ __forceinline__ uint32_t divide(uint32_t x, const Divisor& v) {
+  if (v.d == 1) return x;
+  return (uint32_t)(((uint64_t)x * v.m_hi + (((uint64_t)x * v.m_lo) >> 32)) >> 32);
+}
+
+}  // namespace mhffn

@@ -51,7 +51,7 @@ struct TunedGemmArgs {
   // slices of k each; they leave fp32 partial tiles in P [splits][M][N]
   int splits;
   int64_t slices_per_split;
-  float* P;
+  float* P;         // NULL: one workgroup per tile, which stores C
   int accumulate;   // add to what C holds (one more rounding to bf16)
 };
 
@@ -253,7 +253,7 @@ __global__ __launch_bounds__(64 * G::NW, G::BM == 256 ? 2 : 4) void gemm_bf16_ke
   });
 
   // ---- store: lane = row m, registers = four consecutive n per group ----------------------
-  if (a.splits > 1 || a.accumulate) {
+  if (a.P || a.accumulate) {
 #pragma unroll
     for (int im = 0; im < IM; ++im) {
       const int64_t m = m0 + G::TM * wm + 32 * im + r;
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(64 * G::NW, G::BM == 256 ? 2 : 4) void gemm_bf16_ke
           if (n + 4 > a.N) continue;
           float o[4] = {acc[jn][im][4 * vq], acc[jn][im][4 * vq + 1], acc[jn][im][4 * vq + 2],
                         acc[jn][im][4 * vq + 3]};
-          if (a.splits > 1) {
+          if (a.P) {
             *reinterpret_cast<f32x4*>(a.P + ((size_t)split * a.M + m) * a.N + n) = f32x4{o[0], o[1], o[2], o[3]};
             continue;
           }
@@ -558,7 +558,7 @@ int launch_shape(TunedGemmArgs a, hipStream_t stream) {
   hipLaunchKernelGGL((gemm_bf16_kernel<A_TR, B_TR, G>), dim3((unsigned)xcd_grid_size(a.n_items)), dim3(64 * G::NW),
                      G::kLds, stream, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.splits == 1) return (int)e;
+  if (e != hipSuccess || a.splits == 1 || !a.C) return (int)e;
   const int64_t n4 = a.M * a.N / 4;
   hipLaunchKernelGGL(gemm_bf16_reduce_kernel, dim3((unsigned)((n4 + 255) / 256)), dim3(256), 0,
                      stream, a);
@@ -638,7 +638,7 @@ int launch_gemm_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const voi
   a.tiles_n = 0; a.n_items = 0;
   a.splits = plan.splits;
   a.slices_per_split = plan.slices_per_split;
-  a.P = static_cast<float*>(ws);
+  a.P = plan.splits > 1 ? static_cast<float*>(ws) : nullptr;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (!a_tr && skinny_takes(M, N, K) && !accumulate) {
     if (few_takes(b_tr, M)) return b_tr ? launch_few<true>(a, st) : launch_few<false>(a, st);
@@ -649,6 +649,22 @@ int launch_gemm_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const voi
   if (!a_tr && !b_tr) return launch_form<false, false>(a, plan.shape, st);
   if (a_tr && b_tr) return launch_form<true, true>(a, plan.shape, st);
   return -1;   // transposed A with row-form B: no caller
+}
+
+int launch_gemm_bf16_partials(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb,
+                              float* P, int64_t M, int64_t N, int64_t K, int* splits, void* stream) {
+  const GemmPlan plan = plan_tiles(a_tr, M, N, K);
+  TunedGemmArgs a = {};
+  a.A = static_cast<const uint16_t*>(A);
+  a.B = static_cast<const uint16_t*>(B);
+  a.M = M; a.N = N; a.K = K; a.lda = lda; a.ldb = ldb;
+  a.splits = *splits = plan.splits;
+  a.slices_per_split = plan.slices_per_split;
+  a.P = P;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (!a_tr && b_tr) return launch_form<false, true>(a, plan.shape, st);
+  if (!a_tr && !b_tr) return launch_form<false, false>(a, plan.shape, st);
+  return a_tr && b_tr ? launch_form<true, true>(a, plan.shape, st) : -1;
 }
 
 }  // namespace mhffn

@@ -1,0 +1,152 @@
+// The linear layer Y = R + D(act(X W + b)) and its backward, composed on the host from the
+// library's products and the kernels of pointwise.hip.  Nothing is allocated: operands that the
+// product cannot read where they lie (widths or row strides it does not take) are packed into the
+// workspace, zero-padded, and dZ and the partial products live there too.
+#include "mhffn_internal.h"
+
+namespace mhffn {
+namespace {
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+size_t elt(int dtype) { return dtype == 1 ? 2 : 4; }
+constexpr int64_t kMostLd = 1 << 22;   // (gemm_bf16_supported)
+
+// Workspace, handed out front to back; a null base only adds up
+struct Arena {
+  unsigned char* base;
+  size_t used = 0;
+  void* take(size_t bytes) {
+    void* p = base ? base + used : nullptr;
+    used += align256(bytes);
+    return p;
+  }
+};
+
+// What has to be packed, and the padded sizes of what is
+struct Operands {
+  bool x, w, dz;          // packed X [M][Kp], packed W [Kp][Np], dZ [M][Np] in the workspace
+  int64_t Kp, Np;
+  Operands(const Linear& p, bool backward) {
+    Kp = up(p.K, 32);
+    Np = up(p.N, 32);
+    const bool bf16 = p.dtype == 1;
+    const bool y_fits = p.ldy % 8 == 0 && p.ldy <= kMostLd;
+    x = bf16 && ((backward ? p.K % 8 : p.K % 32) != 0 || p.ldx % 8 != 0 || p.ldx > kMostLd);
+    w = bf16 && (backward ? p.K % 8 != 0 || p.N % 32 != 0 : p.K % 32 != 0 || p.N % 8 != 0);
+    dz = backward && (p.act != 0 || p.drop.threshold != 0 || (bf16 && (p.N % 32 != 0 || !y_fits)));
+  }
+  int64_t ldz(const Linear& p) const { return p.dtype == 1 ? Np : p.N; }
+};
+
+size_t partial_bytes(int dtype, int64_t M, int64_t N, int64_t K) {
+  const size_t one = (size_t)M * N * 4, all = dtype == 1 ? gemm_bf16_workspace_bytes(M, N, K) : 0;
+  return all > one ? all : one;
+}
+
+// C (epilogue e) = A B over the partial products of the tuned kernel, N padded to eight
+int product(int dtype, bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M,
+            int64_t N, int64_t K, float* P, const Epilogue& e, void* stream) {
+  LinearSums s = {P, N, 1};
+  int rc;
+  if (dtype == 1)
+    rc = launch_gemm_bf16_partials(a_tr, b_tr, A, lda, B, ldb, P, M, N, K, &s.splits, stream);
+  else
+    rc = launch_gemm(0, A, a_tr ? 1 : lda, a_tr ? lda : 1, B, b_tr ? 1 : ldb, b_tr ? ldb : 1, P, N, M, N, K, stream);
+  return rc ? rc : launch_linear_epilogue(dtype, s, e, stream);
+}
+
+Epilogue plain(void* Y, int64_t ldy, int64_t M, int64_t N) {
+  Epilogue e = {};
+  e.Y = Y; e.ldy = ldy; e.M = M; e.N = N;
+  return e;
+}
+
+int forward(const Linear& p, const void* X, const void* W, const void* bias, const void* residual, void* Y, void* Z,
+            void* ws, size_t* bytes, void* stream) {
+  const Operands o(p, false);
+  const bool bf16 = p.dtype == 1;
+  Arena arena{static_cast<unsigned char*>(ws)};
+  void* const Xp = o.x ? arena.take((size_t)p.M * o.Kp * 2) : nullptr;
+  void* const Wp = o.w ? arena.take((size_t)o.Kp * o.Np * 2) : nullptr;
+  const int64_t K = o.x || o.w ? o.Kp : p.K, N = bf16 ? up(p.N, 8) : p.N;
+  float* const P = static_cast<float*>(arena.take(partial_bytes(p.dtype, p.M, N, K)));
+  if (bytes) {
+    *bytes = arena.used;
+    return 0;
+  }
+  int rc = 0;
+  if (o.x) rc = launch_pack(p.dtype, X, p.ldx, p.M, p.K, Xp, p.M, o.Kp, stream);
+  if (!rc && o.w) rc = launch_pack(p.dtype, W, p.N, p.K, p.N, Wp, o.Kp, o.Np, stream);
+  if (rc) return rc;
+  Epilogue e = plain(Y, p.ldy, p.M, p.N);
+  e.bias = bias;
+  e.residual = residual; e.ldr = p.ldr;
+  e.Z = Z; e.ldz = p.N;
+  e.act = p.act;
+  e.drop = p.drop;
+  return product(p.dtype, false, true, o.x ? Xp : X, o.x ? o.Kp : p.ldx, o.w ? Wp : W, o.w ? o.Np : p.N, p.M, N, K, P,
+                 e, stream);
+}
+
+int backward(const Linear& p, const void* X, const void* W, const void* Z, const void* dY, void* dX, void* dW,
+             void* dbias, void* ws, size_t* bytes, void* stream) {
+  const Operands o(p, true);
+  const bool bf16 = p.dtype == 1;
+  Arena arena{static_cast<unsigned char*>(ws)};
+  void* const Xp = o.x ? arena.take((size_t)p.M * o.Kp * 2) : nullptr;
+  void* const Wp = o.w ? arena.take((size_t)o.Kp * o.Np * 2) : nullptr;
+  const int64_t ldz = o.ldz(p), K8 = bf16 ? up(p.K, 8) : p.K, N8 = bf16 ? up(p.N, 8) : p.N;
+  const int64_t Nk = bf16 ? o.Np : p.N;   // the contraction of dX
+  void* const dZ = o.dz ? arena.take((size_t)p.M * ldz * elt(p.dtype)) : nullptr;
+  float* const sums = static_cast<float*>(arena.take((size_t)linear_column_blocks(p.M, p.N) * p.N * 4));
+  const size_t px = partial_bytes(p.dtype, p.M, K8, Nk), pw = partial_bytes(p.dtype, K8, N8, p.M);
+  float* const P = static_cast<float*>(arena.take(px > pw ? px : pw));
+  if (bytes) {
+    *bytes = arena.used;
+    return 0;
+  }
+  LinearDz z = {dY, Z, dX || dW ? dZ : nullptr, dbias, sums, p.M, p.N, p.ldy, ldz, p.act, p.drop};
+  int rc = launch_linear_dz(p.dtype, z, stream);
+  if (rc) return rc;
+  const void* const G = o.dz ? dZ : dY;
+  const int64_t ldg = o.dz ? ldz : p.ldy;
+  if (dX) {
+    if (o.w) rc = launch_pack(p.dtype, W, p.N, p.K, p.N, Wp, o.Kp, o.Np, stream);
+    if (!rc) rc = product(p.dtype, false, false, G, ldg, o.w ? Wp : W, o.w ? o.Np : p.N, p.M, K8, Nk, P,
+                          plain(dX, p.ldx, p.M, p.K), stream);
+    if (rc) return rc;
+  }
+  if (dW) {
+    if (o.x) rc = launch_pack(p.dtype, X, p.ldx, p.M, p.K, Xp, p.M, o.Kp, stream);
+    if (!rc) rc = product(p.dtype, true, true, o.x ? Xp : X, o.x ? o.Kp : p.ldx, G, ldg, K8, N8, p.M, P,
+                          plain(dW, p.N, p.K, p.N), stream);
+  }
+  return rc;
+}
+
+}  // namespace
+
+size_t linear_workspace_bytes(const Linear& p, bool back) {
+  size_t bytes = 0;
+  if (p.M == 0) return 0;
+  if (back) backward(p, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, &bytes, nullptr);
+  else forward(p, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, &bytes, nullptr);
+  return bytes;
+}
+
+int launch_linear_forward(const Linear& p, const void* X, const void* W, const void* bias, const void* residual,
+                          void* Y, void* Z, void* ws, void* stream) {
+  return p.M == 0 ? 0 : forward(p, X, W, bias, residual, Y, Z, ws, nullptr, stream);
+}
+
+int launch_linear_backward(const Linear& p, const void* X, const void* W, const void* Z, const void* dY, void* dX,
+                           void* dW, void* dbias, void* ws, void* stream) {
+  if (p.M > 0) return backward(p, X, W, Z, dY, dX, dW, dbias, ws, nullptr, stream);
+  // no rows: the parameters' gradients are zero
+  int rc = dW ? launch_pack(p.dtype, nullptr, 0, 0, 0, dW, p.K, p.N, stream) : 0;
+  if (!rc && dbias) rc = launch_pack(p.dtype, nullptr, 0, 0, 0, dbias, 1, p.N, stream);
+  return rc;
+}
+
+}  // namespace mhffn

@@ -101,20 +101,94 @@ size_t gemm_bf16_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int launch_gemm_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb,
                      void* C, int64_t ldc, int64_t M, int64_t N, int64_t K, void* ws, void* stream,
                      bool accumulate = false);
+// The same product as its fp32 partial sums alone, P [splits][M][N]; returns their number in
+// *splits (at most gemm_bf16_workspace_bytes() / (4 M N), 1 where that is 0).
+int launch_gemm_bf16_partials(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb,
+                              float* P, int64_t M, int64_t N, int64_t K, int* splits, void* stream);
+
+// ---- linear layer with its epilogue, dropout ---------------------------------
+// Dropout after validation: an element stays where its 16 random bits reach `threshold`
+// (0: all stay, the generator is not read; 65536: none does).
+struct Dropout {
+  uint32_t threshold;
+  float scale;           // 65536 / (65536 - threshold)
+  uint64_t call;
+  const uint64_t* rng;   // device: seed, offset
+};
+// Y = residual + D(act(product + bias)), Z = product + bias where kept
+struct Epilogue {
+  const void* bias;      // [N]; may be NULL, like residual and Z
+  const void* residual;
+  void* Z;
+  void* Y;
+  int64_t ldr, ldz, ldy, M, N;
+  int act;               // mhffn_activation
+  int vec;               // bits: rows of Z (1), residual (2), Y (4) are 16-byte aligned
+  Dropout drop;
+};
+struct Linear {
+  int64_t M;             // rows
+  int64_t K, N;          // features in and out
+  int64_t ldx, ldy, ldr; // row strides of X / dX, Y / dY, residual
+  int dtype, act;
+  Dropout drop;
+};
+size_t linear_workspace_bytes(const Linear& p, bool backward);
+int launch_linear_forward(const Linear& p, const void* X, const void* W, const void* bias,
+                          const void* residual, void* Y, void* Z, void* ws, void* stream);
+int launch_linear_backward(const Linear& p, const void* X, const void* W, const void* Z,
+                           const void* dY, void* dX, void* dW, void* dbias, void* ws, void* stream);
+// Y = residual + D(X), X [M][N]; Y may be X or the residual
+int launch_dropout(int dtype, const void* X, int64_t ldx, const Epilogue& e, void* stream);
+// Kernels of pointwise.hip behind the host code of linear.cpp
+struct LinearSums {   // Epilogue over `splits` partial products P [splits][M][ldp]
+  const float* P;
+  int64_t ldp;
+  int splits;
+};
+int launch_linear_epilogue(int dtype, const LinearSums& s, const Epilogue& e, void* stream);
+// [rows][cols] (row stride ld) -> dense [rows_to][cols_to], zero outside
+int launch_pack(int dtype, const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst,
+                int64_t rows_to, int64_t cols_to, void* stream);
+// dZ = D(dY) act'(Z) into dZ [M][ldz] (zero past column N; may be NULL), its column sums into
+// dbias (may be NULL) by way of `partials` (linear_column_blocks(M, N) x N floats)
+struct LinearDz {
+  const void* dY;
+  const void* Z;
+  void* dZ;
+  void* dbias;
+  float* partials;
+  int64_t M, N, ldy, ldz;
+  int act;
+  Dropout drop;
+};
+int64_t linear_column_blocks(int64_t M, int64_t N);
+int launch_linear_dz(int dtype, const LinearDz& a, void* stream);
 
 // ---- whole module: projections around the fused path -------------------------
 // Problem::ldx / ldy are the row strides of the module's input X (dX) and output O (dO);
 // Q and S are dense [N][H*d_h].
+struct Residual {   // the branch O = R + D(S W_out); `rows` may be NULL
+  const void* rows;
+  int64_t ld;
+  Dropout drop;
+};
+size_t module_residual_workspace_bytes(const Problem& p, int dtype, bool backward);
 size_t module_workspace_bytes(const Problem& p, int dtype, bool backward);
 int launch_module_forward(const Problem& p, int dtype, const void* X, const void* W_in,
                           const void* Wg, const void* Wu, const void* Wd, const void* Wr,
                           const void* W_out, void* O, void* Q, void* S, void* ws, size_t ws_bytes,
-                          void* stream);
+                          void* stream, const Residual* residual = nullptr);
 int launch_module_backward(const Problem& p, int dtype, const void* X, const void* W_in,
                            const void* Wg, const void* Wu, const void* Wd, const void* Wr,
                            const void* W_out, const void* Q, const void* S, const void* dO,
                            void* dX, void* dW_in, void* dWg, void* dWu, void* dWd, void* dWr,
                            void* dW_out, void* ws, void* stream);
+int launch_module_residual_backward(const Problem& p, int dtype, const void* X, const void* W_in,
+                                    const void* Wg, const void* Wu, const void* Wd, const void* Wr,
+                                    const void* W_out, const void* Q, const void* S, const void* dO,
+                                    const Dropout& drop, void* dX, void* dW_in, void* dWg, void* dWu,
+                                    void* dWd, void* dWr, void* dW_out, void* ws, void* stream);
 
 // ---- what a call would launch, as text (host only; for tests) ------------------
 // Kernel, tile shape and how the work is shared out, e.g. "pair256 shares=2"; products by form

@@ -59,6 +59,12 @@ int product_tn(int dtype, const void* A, int64_t lda, const void* B, int64_t ldb
   return launch_gemm(dtype, A, 1, lda, B, 1, ldb, C, ldc, M, N, K, stream);
 }
 
+// the output projection with the residual branch in its epilogue
+Linear output_projection(const Problem& p, int dtype, const Residual& r) {
+  const int64_t dm = (int64_t)p.H * p.dh;
+  return {p.N, dm, dm, dm, p.ldy, r.ld, dtype, 0, r.drop};
+}
+
 }  // namespace
 
 std::string module_plan(const Problem& p, int dtype, bool backward) {
@@ -77,10 +83,17 @@ size_t module_workspace_bytes(const Problem& p, int dtype, bool backward) {
   return 2 * act + align256(bwd_workspace_bytes(inner(p), dtype)) + gemm_ws(p, dtype, true);
 }
 
+size_t module_residual_workspace_bytes(const Problem& p, int dtype, bool backward) {
+  if (p.N == 0) return 0;
+  if (backward) return align256(module_workspace_bytes(p, dtype, true)) + align256((size_t)p.N * p.H * p.dh * elt(dtype));
+  const size_t in = gemm_ws(p, dtype, false), out = linear_workspace_bytes(output_projection(p, dtype, {}), false);
+  return align256(fused_fwd_ws(p, dtype)) + (in > out ? in : out);
+}
+
 int launch_module_forward(const Problem& p, int dtype, const void* X, const void* W_in,
                           const void* Wg, const void* Wu, const void* Wd, const void* Wr,
                           const void* W_out, void* O, void* Q, void* S, void* ws, size_t ws_bytes,
-                          void* stream) {
+                          void* stream, const Residual* residual) {
   if (p.N == 0) return 0;
   const int64_t dm = (int64_t)p.H * p.dh;
   const Problem q = inner(p);
@@ -92,6 +105,12 @@ int launch_module_forward(const Problem& p, int dtype, const void* X, const void
   e = dtype == 1 ? launch_fwd_bf16(q, Q, Wg, Wu, Wd, Wr, S, ws, stream)
                  : launch_fwd_f32(q, Q, Wg, Wu, Wd, Wr, S, ws, ws_bytes, stream);
   if (e) return e;
+  if (residual) {
+    // O = R + D(S W_out)
+    void* const lws = static_cast<unsigned char*>(ws) + align256(fused_fwd_ws(p, dtype));
+    const Linear out = output_projection(p, dtype, *residual);
+    return launch_linear_forward(out, S, W_out, nullptr, residual->rows, O, nullptr, lws, stream);
+  }
   // O[l][j] = sum_i S[l][i] W_out[i][j]
   return product_nn(dtype, S, dm, W_out, dm, O, p.ldy, p.N, dm, dm, gws, stream);
 }
@@ -137,6 +156,27 @@ int launch_module_backward(const Problem& p, int dtype, const void* X, const voi
   // dX[l][i] = sum_j dQ[l][j] W_in[i][j]
   if (dX) e = product_nt(dtype, dQ, dm, W_in, dm, dX, p.ldx, p.N, dm, dm, gws, stream);
   return e;
+}
+
+int launch_module_residual_backward(const Problem& p, int dtype, const void* X, const void* W_in,
+                                    const void* Wg, const void* Wu, const void* Wd, const void* Wr,
+                                    const void* W_out, const void* Q, const void* S, const void* dO,
+                                    const Dropout& drop, void* dX, void* dW_in, void* dWg, void* dWu,
+                                    void* dWd, void* dWr, void* dW_out, void* ws, void* stream) {
+  Problem q = p;
+  if (drop.threshold != 0 && p.N > 0) {
+    const int64_t dm = (int64_t)p.H * p.dh;
+    void* const G = static_cast<unsigned char*>(ws) + align256(module_workspace_bytes(p, dtype, true));
+    Epilogue e = {};
+    e.Y = G; e.ldy = dm; e.M = p.N; e.N = dm;
+    e.drop = drop;
+    const int rc = launch_dropout(dtype, dO, p.ldy, e, stream);
+    if (rc) return rc;
+    dO = G;
+    q.ldy = dm;
+  }
+  return launch_module_backward(q, dtype, X, W_in, Wg, Wu, Wd, Wr, W_out, Q, S, dO, dX, dW_in, dWg, dWu, dWd, dWr,
+                                dW_out, ws, stream);
 }
 
 }  // namespace mhffn

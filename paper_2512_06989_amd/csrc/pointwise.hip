@@ -1,0 +1,222 @@
+// Kernels of the linear layer and of dropout that touch every element once: the epilogue over
+// partial products, dZ with the sums of its columns, dropout alone, and operands packed for the
+// product.  All of them move pieces of eight columns (epilogue.h) and are bound by memory.
+#include "epilogue.h"
+
+namespace mhffn {
+namespace {
+
+constexpr int kThreads = 256;
+
+// A thread's pieces of a [rows][cols] array, in row order: piece -> (row, first column)
+struct Pieces {
+  int64_t total;      // rows * per_row
+  uint32_t per_row;
+  Divisor div;
+};
+Pieces make_pieces(int64_t rows, int64_t cols) {
+  const uint32_t per = (uint32_t)((cols + 7) / 8);
+  return {rows * (int64_t)per, per, make_divisor(per)};
+}
+__device__ __forceinline__ void piece_at(const Pieces& p, int64_t i, int64_t& row, int64_t& col) {
+  row = p.total <= 0xFFFFFFFFll ? (int64_t)divide((uint32_t)i, p.div) : i / p.per_row;
+  col = 8 * (i - row * p.per_row);
+}
+// (a launch holds fewer than 2^32 threads: past that a thread takes several pieces)
+unsigned piece_blocks(const Pieces& p) {
+  const int64_t blocks = (p.total + kThreads - 1) / kThreads;
+  return (unsigned)(blocks < (1 << 20) ? blocks : 1 << 20);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void linear_epilogue_kernel(LinearSums s, Epilogue e, Pieces p) {
+  const DropKey key = drop_key(e.drop);
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < p.total; i += (int64_t)gridDim.x * kThreads) {
+    int64_t row, col;
+    piece_at(p, i, row, col);
+    const int cols = (int)(s.ldp - col < 8 ? s.ldp - col : 8);
+    float v[8];
+    load8(s.P + row * s.ldp + col, cols, (s.ldp & 3) == 0, v);
+    for (int k = 1; k < s.splits; ++k) {
+      float w[8];
+      load8(s.P + ((int64_t)k * e.M + row) * s.ldp + col, cols, (s.ldp & 3) == 0, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += w[j];
+    }
+    epilogue8<T>(v, row, col, e, key);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void dropout_kernel(const T* X, int64_t ldx, bool vec_x, Epilogue e, Pieces p) {
+  const DropKey key = drop_key(e.drop);
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < p.total; i += (int64_t)gridDim.x * kThreads) {
+    int64_t row, col;
+    piece_at(p, i, row, col);
+    float v[8];
+    load8(X + row * ldx + col, (int)(e.N - col < 8 ? e.N - col : 8), vec_x, v);
+    epilogue8<T>(v, row, col, e, key);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void pack_kernel(const T* src, int64_t ld, bool vec, int64_t rows, int64_t cols,
+                                                        T* dst, int64_t cols_to, Pieces p) {
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < p.total; i += (int64_t)gridDim.x * kThreads) {
+    int64_t row, col;
+    piece_at(p, i, row, col);
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (row < rows && col < cols) load8(src + row * ld + col, (int)(cols - col < 8 ? cols - col : 8), vec, v);
+    store8(dst + row * cols_to + col, (int)(cols_to - col < 8 ? cols_to - col : 8), (cols_to & 7) == 0, v);
+  }
+}
+
+// Lane t of a workgroup takes piece column t % lanes of rows t / lanes, + rows_at_once, ..: the
+// workgroup's share of dZ, and the sums of its eight columns per lane, which meet in LDS in row
+// order and go out as one partial sum per column and row block.
+struct DzGrid {
+  int lane_shift;        // log2 of the piece columns a workgroup spans
+  int64_t pieces;        // piece columns, padding of dZ among them
+  int64_t rows_per_block;
+};
+template <typename T>
+__global__ __launch_bounds__(kThreads) void linear_dz_kernel(LinearDz a, DzGrid g, int vec) {
+  __shared__ float sums[kThreads * 8];
+  const DropKey key = drop_key(a.drop);
+  const int lanes = 1 << g.lane_shift, at_once = kThreads >> g.lane_shift;
+  const int lane = threadIdx.x & (lanes - 1), first = threadIdx.x >> g.lane_shift;
+  const int64_t piece = (int64_t)blockIdx.x * lanes + lane, col = 8 * piece;
+  const int64_t r0 = (int64_t)blockIdx.y * g.rows_per_block;
+  const int64_t r1 = r0 + g.rows_per_block < a.M ? r0 + g.rows_per_block : a.M;
+  const int64_t per_row = (a.N + 7) >> 3;
+  const int cols = (int)(a.N - col < 8 ? a.N - col : 8);   // (0 or less: padding)
+  float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (piece < g.pieces) {
+    for (int64_t row = r0 + first; row < r1; row += at_once) {
+      float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      if (cols > 0) {
+        load8(static_cast<const T*>(a.dY) + row * a.ldy + col, cols, vec & 1, v);
+        drop8(v, (uint64_t)row * per_row + piece, a.drop, key);
+        if (a.act) {
+          float z[8];
+          load8(static_cast<const T*>(a.Z) + row * a.N + col, cols, vec & 2, z);
+          slope8(v, z, a.act);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += v[j];
+      }
+      if (a.dZ) store8(static_cast<T*>(a.dZ) + row * a.ldz + col, (int)(a.ldz - col < 8 ? a.ldz - col : 8), vec & 4, v);
+    }
+  }
+  if (!a.dbias) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sums[threadIdx.x * 8 + j] = acc[j];
+  __syncthreads();
+  for (int t = threadIdx.x; t < 8 * lanes; t += kThreads) {
+    float sum = 0.f;
+    for (int k = 0; k < at_once; ++k) sum += sums[k * 8 * lanes + t];
+    const int64_t c = (int64_t)blockIdx.x * 8 * lanes + t;
+    if (c < a.N) a.partials[(int64_t)blockIdx.y * a.N + c] = sum;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void column_sum_kernel(const float* partials, int64_t blocks, int64_t N, T* out) {
+  const int64_t c = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (c >= N) return;
+  float sum = 0.f;
+  for (int64_t b = 0; b < blocks; ++b) sum += partials[b * N + c];
+  if constexpr (sizeof(T) == 2) out[c] = (uint16_t)pack_bf16(sum, 0.f);
+  else out[c] = sum;
+}
+
+inline bool vec_rows(const void* p, int64_t ld, int dtype) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % (dtype == 1 ? 8 : 4) == 0;
+}
+Epilogue with_vec(Epilogue e, int dtype) {
+  e.vec = (vec_rows(e.Z, e.ldz, dtype) ? 1 : 0) | (vec_rows(e.residual, e.ldr, dtype) ? 2 : 0) |
+          (vec_rows(e.Y, e.ldy, dtype) ? 4 : 0);
+  return e;
+}
+
+DzGrid dz_grid(int64_t M, int64_t N, int64_t cols_to) {
+  DzGrid g;
+  g.pieces = ((cols_to > N ? cols_to : N) + 7) / 8;
+  g.lane_shift = 0;
+  while (g.lane_shift < 5 && (1 << g.lane_shift) < (N + 7) / 8) ++g.lane_shift;
+  const int64_t blocks = linear_column_blocks(M, N);
+  g.rows_per_block = (M + blocks - 1) / blocks;
+  return g;
+}
+
+}  // namespace
+
+int64_t linear_column_blocks(int64_t M, int64_t N) {
+  const int64_t across = (N + 255) / 256, want = 2048 / across > 1 ? 2048 / across : 1;
+  const int64_t most = (M + 7) / 8;
+  return most < want ? (most > 0 ? most : 1) : want;
+}
+
+int launch_linear_epilogue(int dtype, const LinearSums& s, const Epilogue& e0, void* stream) {
+  const Epilogue e = with_vec(e0, dtype);
+  const Pieces p = make_pieces(e.M, e.N);
+  if (p.total == 0) return 0;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == 1) hipLaunchKernelGGL(linear_epilogue_kernel<uint16_t>, dim3(piece_blocks(p)), dim3(kThreads), 0, st, s, e, p);
+  else hipLaunchKernelGGL(linear_epilogue_kernel<float>, dim3(piece_blocks(p)), dim3(kThreads), 0, st, s, e, p);
+  return (int)hipGetLastError();
+}
+
+int launch_dropout(int dtype, const void* X, int64_t ldx, const Epilogue& e0, void* stream) {
+  const Epilogue e = with_vec(e0, dtype);
+  const Pieces p = make_pieces(e.M, e.N);
+  if (p.total == 0) return 0;
+  const bool vec = vec_rows(X, ldx, dtype);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == 1)
+    hipLaunchKernelGGL(dropout_kernel<uint16_t>, dim3(piece_blocks(p)), dim3(kThreads), 0, st,
+                       static_cast<const uint16_t*>(X), ldx, vec, e, p);
+  else
+    hipLaunchKernelGGL(dropout_kernel<float>, dim3(piece_blocks(p)), dim3(kThreads), 0, st,
+                       static_cast<const float*>(X), ldx, vec, e, p);
+  return (int)hipGetLastError();
+}
+
+int launch_pack(int dtype, const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t rows_to,
+                int64_t cols_to, void* stream) {
+  const Pieces p = make_pieces(rows_to, cols_to);
+  if (p.total == 0) return 0;
+  const bool vec = vec_rows(src, ld, dtype);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == 1)
+    hipLaunchKernelGGL(pack_kernel<uint16_t>, dim3(piece_blocks(p)), dim3(kThreads), 0, st,
+                       static_cast<const uint16_t*>(src), ld, vec, rows, cols, static_cast<uint16_t*>(dst), cols_to, p);
+  else
+    hipLaunchKernelGGL(pack_kernel<float>, dim3(piece_blocks(p)), dim3(kThreads), 0, st,
+                       static_cast<const float*>(src), ld, vec, rows, cols, static_cast<float*>(dst), cols_to, p);
+  return (int)hipGetLastError();
+}
+
+int launch_linear_dz(int dtype, const LinearDz& a, void* stream) {
+  if (!a.dZ && !a.dbias) return 0;
+  const DzGrid g = dz_grid(a.M, a.N, a.dZ ? a.ldz : a.N);
+  const int64_t blocks = linear_column_blocks(a.M, a.N);
+  const int vec = (vec_rows(a.dY, a.ldy, dtype) ? 1 : 0) | (vec_rows(a.Z, a.N, dtype) ? 2 : 0) |
+                  (vec_rows(a.dZ, a.ldz, dtype) ? 4 : 0);
+  const dim3 grid((unsigned)((g.pieces + (1 << g.lane_shift) - 1) >> g.lane_shift), (unsigned)blocks);
+  const dim3 sum_grid((unsigned)((a.N + kThreads - 1) / kThreads));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == 1) hipLaunchKernelGGL(linear_dz_kernel<uint16_t>, grid, dim3(kThreads), 0, st, a, g, vec);
+  else hipLaunchKernelGGL(linear_dz_kernel<float>, grid, dim3(kThreads), 0, st, a, g, vec);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.dbias) return (int)e;
+  if (dtype == 1)
+    hipLaunchKernelGGL(column_sum_kernel<uint16_t>, sum_grid, dim3(kThreads), 0, st, a.partials, blocks, a.N,
+                       static_cast<uint16_t*>(a.dbias));
+  else
+    hipLaunchKernelGGL(column_sum_kernel<float>, sum_grid, dim3(kThreads), 0, st, a.partials, blocks, a.N,
+                       static_cast<float*>(a.dbias));
+  return (int)hipGetLastError();
+}
+
+}  // namespace mhffn

@@ -19,9 +19,14 @@ F32, BF16 = 0, 1
 ROUTE_PARAMS, ROUTE_WEIGHTS = 0, 1
 OP_FORWARD, OP_BACKWARD, OP_UNFUSED_FORWARD, OP_UNFUSED_BACKWARD = 0, 1, 2, 3
 OP_MODULE_FORWARD, OP_MODULE_BACKWARD = 4, 5
+OP_MODULE_RESIDUAL_FORWARD, OP_MODULE_RESIDUAL_BACKWARD = 6, 7
+OP_LINEAR_FORWARD, OP_LINEAR_BACKWARD = 8, 9
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 EXPORTS = ("mhffn_workspace_bytes", "mhffn_forward", "mhffn_backward", "mhffn_backward_phases",
            "mhffn_reference_unfused", "mhffn_module_forward", "mhffn_module_backward",
-           "mhffn_status_string", "mhffn_version", "mhffn_init", "mhffn_forward_static")
+           "mhffn_status_string", "mhffn_version", "mhffn_init", "mhffn_forward_static",
+           "mhffn_linear_workspace_bytes", "mhffn_linear_forward", "mhffn_linear_backward", "mhffn_dropout",
+           "mhffn_module_residual_forward", "mhffn_module_residual_backward")
 
 
 class Desc(ctypes.Structure):
@@ -31,6 +36,21 @@ class Desc(ctypes.Structure):
                 ("d_sub", ctypes.c_int32), ("ld_x", ctypes.c_int64),
                 ("ld_y", ctypes.c_int64), ("dtype", ctypes.c_int32),
                 ("route_mode", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class LinearDesc(ctypes.Structure):
+    """Mirror of `mhffn_linear_desc`."""
+    _fields_ = [("n_rows", ctypes.c_int64), ("d_in", ctypes.c_int32), ("d_out", ctypes.c_int32),
+                ("ld_x", ctypes.c_int64), ("ld_y", ctypes.c_int64), ("ld_r", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("dropout", ctypes.c_float),
+                ("call", ctypes.c_uint64)]
+
+
+class DropoutDesc(ctypes.Structure):
+    """Mirror of `mhffn_dropout_desc`."""
+    _fields_ = [("n_rows", ctypes.c_int64), ("n_cols", ctypes.c_int32), ("ld_x", ctypes.c_int64),
+                ("ld_y", ctypes.c_int64), ("ld_r", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("dropout", ctypes.c_float), ("call", ctypes.c_uint64)]
 
 
 class MhffnError(RuntimeError):
@@ -70,6 +90,20 @@ def load():
     lib.mhffn_module_forward.restype = ctypes.c_int
     lib.mhffn_module_backward.argtypes = [dp] + [vp] * 17 + [vp, sz, vp]
     lib.mhffn_module_backward.restype = ctypes.c_int
+    u64, f32 = ctypes.c_uint64, ctypes.c_float
+    lp = ctypes.POINTER(LinearDesc)
+    lib.mhffn_linear_workspace_bytes.argtypes = [lp, ctypes.c_int]
+    lib.mhffn_linear_workspace_bytes.restype = sz
+    lib.mhffn_linear_forward.argtypes = [lp] + [vp] * 7 + [vp, sz, vp]
+    lib.mhffn_linear_forward.restype = ctypes.c_int
+    lib.mhffn_linear_backward.argtypes = [lp] + [vp] * 8 + [vp, sz, vp]
+    lib.mhffn_linear_backward.restype = ctypes.c_int
+    lib.mhffn_dropout.argtypes = [ctypes.POINTER(DropoutDesc)] + [vp] * 4 + [vp]
+    lib.mhffn_dropout.restype = ctypes.c_int
+    lib.mhffn_module_residual_forward.argtypes = [dp] + [vp] * 8 + [ctypes.c_int64, f32, vp, u64] + [vp] * 3 + [vp, sz, vp]
+    lib.mhffn_module_residual_forward.restype = ctypes.c_int
+    lib.mhffn_module_residual_backward.argtypes = [dp] + [vp] * 10 + [f32, vp, u64] + [vp] * 7 + [vp, sz, vp]
+    lib.mhffn_module_residual_backward.restype = ctypes.c_int
     lib.mhffn_status_string.argtypes = [ctypes.c_int]
     lib.mhffn_status_string.restype = ctypes.c_char_p
     lib.mhffn_version.restype = ctypes.c_char_p
@@ -303,16 +337,141 @@ def reference_unfused(X, W_gate, W_up, W_down, route, eps=1e-6, route_mode=ROUTE
     return Y, {k: out[k] for k in want}
 
 
+def _matrix_rows(name, t, shape, like):
+    """Check a row tensor of `shape` with unit column stride, dtype and device of `like`; returns its
+    row stride in elements (its width for fewer than two rows)."""
+    _require(tuple(t.shape) == tuple(shape), "%s must be %s, got %s" % (name, list(shape), tuple(t.shape)))
+    _require(t.dtype == like.dtype, "%s has dtype %s, expected %s" % (name, t.dtype, like.dtype))
+    _require(t.device == like.device, "%s is on %s, expected %s" % (name, t.device, like.device))
+    _require(t.shape[0] == 0 or t.shape[1] == 1 or t.stride(1) == 1, "%s rows must be contiguous" % name)
+    if t.shape[0] < 2:
+        return t.shape[1]
+    _require(t.stride(0) >= t.shape[1], "%s rows overlap (row stride %d)" % (name, t.stride(0)))
+    return t.stride(0)
+
+
+def _check_dropout(dropout, rng, call, device):
+    _require(0.0 <= float(dropout) <= 1.0, "dropout must be within 0 .. 1, got %r" % (dropout,))
+    _require(0 <= int(call) < 1 << 64, "call must be within 0 .. 2^64 - 1, got %r" % (call,))
+    if rng is not None:
+        _dense("rng", rng, (2,), torch.int64, device)
+
+
+def _check_device(X):
+    _require(X.is_cuda, "X is on %s: the kernels take device memory" % X.device)
+    _require(X.device.index == torch.cuda.current_device(),
+             "X is on %s, the current device is cuda:%d" % (X.device, torch.cuda.current_device()))
+
+
+def _check_branch(X, residual, dropout, rng, call):
+    _check_dropout(dropout, rng, call, X.device)
+    if residual is not None:
+        _matrix_rows("residual", residual, X.shape, X)
+    if residual is not None or dropout:
+        _check_device(X)
+
+
+def _check_linear(X, W):
+    _require(X.dim() == 2, "X must be [N, d_in], got %s" % (tuple(X.shape),))
+    _dtype_code(X)
+    _matrix_rows("X", X, X.shape, X)
+    _require(W.dim() == 2, "W must be [d_in, d_out], got %s" % (tuple(W.shape),))
+    _dense("W", W, (X.shape[1], W.shape[1]), X.dtype, X.device)
+
+
+def linear_forward(X, W, bias=None, residual=None, activation=ACT_NONE, dropout=0.0, rng=None, call=0, save=False,
+                   out=None, stream=None, workspace=None):
+    """Linear layer with its epilogue: Z = X W + bias; Y = residual + D(activation(Z)).
+
+    X [N, d_in] and residual [N, d_out] may be row-strided, W [d_in, d_out] and bias [d_out] are
+    dense; every width is taken.  `activation`: ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU.  D: dropout()
+    with probability `dropout`.  Returns Y, or (Y, Z) with `save`: linear_backward needs Z of an
+    activation.  `out`: tensors to write, under "Y" and "Z"; Y may be the residual itself."""
+    r = (_host or _load_host()).linear_forward(X, W, bias, residual, int(activation), dropout, rng, call, bool(save),
+                                               dict(out) if out else None, _raw(stream), workspace)
+    if r is None:
+        _check_linear(X, W)
+        out, shape = dict(out or {}), (X.shape[0], W.shape[1])
+        if bias is not None:
+            _dense("bias", bias, shape[1:], X.dtype, X.device)
+        for k, t in (("residual", residual), ("Y", out.get("Y"))):
+            if t is not None:
+                _matrix_rows(k, t, shape, X)
+        if out.get("Z") is not None:
+            _dense("Z", out["Z"], shape, X.dtype, X.device)
+        _check_dropout(dropout, rng, call, X.device)
+        _check_device(X)
+        raise ValueError("linear_forward: invalid arguments")
+    return _result(r, "mhffn_linear_forward")
+
+
+LINEAR_GRADS = ("dX", "dW", "dbias")
+
+
+def linear_backward(X, W, dY, Z=None, activation=ACT_NONE, dropout=0.0, rng=None, call=0, want=LINEAR_GRADS,
+                    out=None, stream=None, workspace=None):
+    """Backward of linear_forward, whose activation, dropout, rng and call it is given, from X, W, dY
+    and, for an activation, Z.  Returns a dict of the gradients in `want`; dX has X's row stride.
+    The gradient of the residual is dY itself."""
+    want = tuple(want)
+    r = (_host or _load_host()).linear_backward(X, W, dY, Z, int(activation), dropout, rng, call, want,
+                                                dict(out) if out else None, _raw(stream), workspace)
+    if r is None:
+        _check_linear(X, W)
+        out, shape = dict(out or {}), (X.shape[0], W.shape[1])
+        _matrix_rows("dY", dY, shape, X)
+        if Z is not None:
+            _dense("Z", Z, shape, X.dtype, X.device)
+        for k in want:
+            if k not in LINEAR_GRADS:
+                raise KeyError(k)
+        if out.get("dX") is not None:
+            _require(_matrix_rows("dX", out["dX"], X.shape, X) == _matrix_rows("X", X, X.shape, X),
+                     "dX must have X's row stride")
+        for k, t in (("dW", W.shape), ("dbias", shape[1:])):
+            if out.get(k) is not None:
+                _dense(k, out[k], t, X.dtype, X.device)
+        _check_dropout(dropout, rng, call, X.device)
+        _check_device(X)
+        raise ValueError("linear_backward: invalid arguments")
+    r = _result(r, "mhffn_linear_backward")
+    return {k: r[k] for k in want}
+
+
+def dropout(X, p, rng, call=0, residual=None, out=None, stream=None):
+    """Y = residual + D(X) on [N, n] rows: D drops an element with probability p (in steps of 2^-16) and
+    scales what stays.  Returns Y; `out` may be X or the residual.
+
+    Which elements stay follows from `rng`, an int64 tensor (seed, offset) on X's device, the number
+    `call` and the element's place alone (Philox4x32-10, see mhffn.h) and is never stored: the
+    backward is the same call on dY, without the residual.  The kernels read rng when they run, so a
+    captured graph draws new numbers once the offset has been advanced."""
+    r = (_host or _load_host()).dropout(X, p, rng, call, residual, out, _raw(stream))
+    if r is None:
+        _require(X.dim() == 2, "X must be [N, n], got %s" % (tuple(X.shape),))
+        _dtype_code(X)
+        for k, t in (("X", X), ("residual", residual), ("out", out)):
+            if t is not None:
+                _matrix_rows(k, t, X.shape, X)
+        _check_dropout(p, rng, call, X.device)
+        _check_device(X)
+        raise ValueError("dropout: invalid arguments")
+    return _result(r, "mhffn_dropout")
+
+
 MODULE_GRADS = ("dX", "dW_in", "dW_gate", "dW_up", "dW_down", "dW_r", "dW_out")
 
 
 def module_forward(X, W_in, W_gate, W_up, W_down, W_r, W_out, eps=1e-6, out=None, stream=None,
-                   workspace=None):
+                   workspace=None, residual=None, dropout=0.0, rng=None, call=0):
     """The whole module: O = fused(X W_in) W_out.  Returns (O, Q, S); Q and S are the two
-    d_model-wide activations that module_backward needs."""
+    d_model-wide activations that module_backward needs.  With a `residual` ([N, d_model]) or a
+    `dropout` the residual branch around it: O = residual + D(fused(X W_in) W_out), see dropout()."""
     r = (_host or _load_host()).module_forward(X, W_in, W_gate, W_up, W_down, W_r, W_out, eps,
-                                               dict(out) if out else None, _raw(stream), workspace)
+                                               dict(out) if out else None, _raw(stream), workspace,
+                                               residual, dropout, rng, call)
     if r is None:
+        _check_branch(X, residual, dropout, rng, call)
         _check_params(X, W_gate, W_up, W_down, W_r, ROUTE_PARAMS)
         out, (N, dm) = dict(out or {}), X.shape
         for k, w in (("W_in", W_in), ("W_out", W_out)):
@@ -326,12 +485,15 @@ def module_forward(X, W_in, W_gate, W_up, W_down, W_r, W_out, eps=1e-6, out=None
 
 
 def module_backward(X, W_in, W_gate, W_up, W_down, W_r, W_out, Q, S, dO, eps=1e-6,
-                    want=MODULE_GRADS, out=None, stream=None, workspace=None):
-    """Backward of module_forward from the saved Q and S.  Returns a dict of gradients."""
+                    want=MODULE_GRADS, out=None, stream=None, workspace=None, dropout=0.0, rng=None, call=0):
+    """Backward of module_forward from the saved Q and S.  Returns a dict of gradients.  `dropout`,
+    `rng` and `call` are those of the forward; the gradient of its residual is dO itself."""
     want = tuple(want)
     r = (_host or _load_host()).module_backward(X, W_in, W_gate, W_up, W_down, W_r, W_out, Q, S, dO, eps,
-                                                want, dict(out) if out else None, _raw(stream), workspace)
+                                                want, dict(out) if out else None, _raw(stream), workspace,
+                                                dropout, rng, call)
     if r is None:
+        _check_branch(X, None, dropout, rng, call)
         _check_params(X, W_gate, W_up, W_down, W_r, ROUTE_PARAMS)
         out, (N, dm) = dict(out or {}), X.shape
         like = {"dW_in": W_in, "dW_gate": W_gate, "dW_up": W_up, "dW_down": W_down,
