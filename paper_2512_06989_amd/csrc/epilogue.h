@@ -150,28 +150,58 @@ __device__ __forceinline__ void store8(float* p, int cols, bool vec, const float
   }
 }
 
-// ---- the epilogue of one piece ---------------------------------------------------------------------
-// v: the product's eight sums in, what was stored in Y out.  The residual is read before Y is
-// written, by the same thread: Y may be the residual itself.
+// ---- the epilogue of pieces in one column of pieces -------------------------------------------------
+// Columns col .. col + 7 of any row, whose bias is read once.  residual() before finish(), by the
+// same thread: Y may be the residual itself.  Rows and columns that do not exist are left alone.
+template <typename T>
+struct EpilogueColumns {
+  int64_t col;
+  int cols;            // how many of the eight exist (0 or less: none)
+  float bias[8];
+  __device__ __forceinline__ EpilogueColumns(const Epilogue& e, int64_t col_) : col(col_) {
+    cols = (int)(e.N - col < 8 ? e.N - col : 8);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) bias[j] = 0.f;
+    if (e.bias && cols > 0) load8(static_cast<const T*>(e.bias) + col, cols, true, bias);
+  }
+  __device__ __forceinline__ void residual(int64_t row, const Epilogue& e, float (&r)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = 0.f;
+    if (e.residual && row < e.M && cols > 0) load8(static_cast<const T*>(e.residual) + row * e.ldr + col, cols, e.vec & 2, r);
+  }
+  // v: the product's eight sums in, what was stored in Y out
+  __device__ __forceinline__ void finish(float (&v)[8], int64_t row, const float (&r)[8], const Epilogue& e, const DropKey& key) const {
+    if (row >= e.M || cols <= 0) return;
+    if (e.bias) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += bias[j];
+    }
+    if (e.Z) store8(static_cast<T*>(e.Z) + row * e.ldz + col, cols, e.vec & 1, v);
+    activate8(v, e.act);
+    drop8(v, (uint64_t)row * (uint64_t)((e.N + 7) >> 3) + (uint64_t)(col >> 3), e.drop, key);
+    if (e.residual) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += r[j];
+    }
+    store8(static_cast<T*>(e.Y) + row * e.ldy + col, cols, e.vec & 4, v);
+  }
+};
 template <typename T>
 __device__ __forceinline__ void epilogue8(float (&v)[8], int64_t row, int64_t col, const Epilogue& e, const DropKey& key) {
-  const int cols = (int)(e.N - col < 8 ? e.N - col : 8);
-  if (e.bias) {
-    float b[8];
-    load8(static_cast<const T*>(e.bias) + col, cols, true, b);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += b[j];
-  }
-  if (e.Z) store8(static_cast<T*>(e.Z) + row * e.ldz + col, cols, e.vec & 1, v);
-  activate8(v, e.act);
-  drop8(v, (uint64_t)row * (uint64_t)((e.N + 7) >> 3) + (uint64_t)(col >> 3), e.drop, key);
-  if (e.residual) {
-    float r[8];
-    load8(static_cast<const T*>(e.residual) + row * e.ldr + col, cols, e.vec & 2, r);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += r[j];
-  }
-  store8(static_cast<T*>(e.Y) + row * e.ldy + col, cols, e.vec & 4, v);
+  const EpilogueColumns<T> ec(e, col);
+  float r[8];
+  ec.residual(row, e, r);
+  ec.finish(v, row, r, e, key);
+}
+
+// Host: which row tensors move whole pieces
+inline bool vec_rows(const void* p, int64_t ld, int dtype) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % (dtype == 1 ? 8 : 4) == 0;
+}
+inline Epilogue with_vec(Epilogue e, int dtype) {
+  e.vec = (vec_rows(e.Z, e.ldz, dtype) ? 1 : 0) | (vec_rows(e.residual, e.ldr, dtype) ? 2 : 0) |
+          (vec_rows(e.Y, e.ldy, dtype) ? 4 : 0);
+  return e;
 }
 
 // ---- division by a number that the host knows ----------------------------------------------------------

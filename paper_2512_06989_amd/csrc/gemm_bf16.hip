@@ -31,8 +31,7 @@
 // on two stages of 64: 136 .. 162), 16384 x 1024 x 1024 42 us (54), 4000 x 2048 x 2048 41 us
 // (62 with its partials), 1000 x 2048 x 2048 19 us (33); weight gradient of 16384 rows,
 // 1024 x 1024: 60 us (71).
-#include "mhffn_device.h"
-#include "mhffn_internal.h"
+#include "epilogue.h"
 
 #include <type_traits>
 
@@ -82,8 +81,12 @@ using Tile64x128 = GemmTile<64, 128, 2, 2, 5>;   // (m side in row form: a trans
 // byte offset of 16-byte chunk `chunk` of `row` in a row-form image
 __device__ __forceinline__ int row_image_off(int row, int chunk) { return row * 64 + ((chunk ^ ((row >> 2) & 3)) << 4); }
 
-template <bool A_TR, bool B_TR, typename G>
-__global__ __launch_bounds__(64 * G::NW, G::BM == 256 ? 2 : 4) void gemm_bf16_kernel(TunedGemmArgs a) {
+// What a product's kernel does with its sums: stores them in C (or adds to it), or the linear layer's epilogue
+struct NoEpilogue {};
+template <typename E> constexpr bool kLinear = std::is_same<E, Epilogue>::value;
+
+template <bool A_TR, bool B_TR, typename G, typename E>
+__global__ __launch_bounds__(64 * G::NW, G::BM == 256 ? 2 : 4) void gemm_bf16_kernel(TunedGemmArgs a, E e) {
   constexpr int IM = G::IM, IN = G::IN, S = G::S, NW = G::NW;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -253,6 +256,41 @@ __global__ __launch_bounds__(64 * G::NW, G::BM == 256 ? 2 : 4) void gemm_bf16_ke
   });
 
   // ---- store: lane = row m, registers = four consecutive n per group ----------------------
+  if constexpr (kLinear<E>) {
+    // The sums pass through LDS in fp32, 32 rows of the wave's piece at a time (16-byte chunks of a
+    // row permuted by the row), so that a lane holds eight columns of one row: whole rows of the
+    // residual, Z and Y move, and a call of the generator serves the lane that makes it.
+    constexpr int CH = G::TN / 4, LPR = G::TN / 8, RPP = 64 / LPR, PASSES = 32 / RPP;
+    const DropKey key = drop_key(e.drop);
+    __syncthreads();                                   // the stages are done with
+    unsigned char* piece = smem + wave * (32 * G::TN * 4);
+    const int64_t n = n0 + G::TN * wn + 8 * (lane % LPR);
+    EpilogueColumns<uint16_t> ec(e, n);
+#pragma unroll
+    for (int im = 0; im < IM; ++im) {
+      const int64_t mb = m0 + G::TM * wm + 32 * im;
+      float res[PASSES][8];
+#pragma unroll
+      for (int q = 0; q < PASSES; ++q) ec.residual(mb + q * RPP + lane / LPR, e, res[q]);
+#pragma unroll
+      for (int jn = 0; jn < IN; ++jn)
+#pragma unroll
+        for (int vq = 0; vq < 4; ++vq)
+          *reinterpret_cast<f32x4*>(piece + r * (G::TN * 4) + (((8 * jn + 2 * vq + g) ^ (r & (CH - 1))) << 4)) =
+              f32x4{acc[jn][im][4 * vq], acc[jn][im][4 * vq + 1], acc[jn][im][4 * vq + 2], acc[jn][im][4 * vq + 3]};
+      __builtin_amdgcn_wave_barrier();                 // (the piece is this wave's own: one queue)
+#pragma unroll
+      for (int q = 0; q < PASSES; ++q) {
+        const int row = q * RPP + lane / LPR, c = 2 * (lane % LPR);
+        const f32x4 lo4 = *reinterpret_cast<const f32x4*>(piece + row * (G::TN * 4) + ((c ^ (row & (CH - 1))) << 4));
+        const f32x4 hi4 = *reinterpret_cast<const f32x4*>(piece + row * (G::TN * 4) + (((c + 1) ^ (row & (CH - 1))) << 4));
+        float v[8] = {lo4[0], lo4[1], lo4[2], lo4[3], hi4[0], hi4[1], hi4[2], hi4[3]};
+        ec.finish(v, mb + row, res[q], e, key);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    return;
+  }
   if (a.P || a.accumulate) {
 #pragma unroll
     for (int im = 0; im < IM; ++im) {
@@ -353,8 +391,8 @@ constexpr int kSkinnyLds = kSkinnyWaves * kSkinnyWaveLds;
 constexpr int kSkinnyK = 64;               // k per slice of this kernel
 constexpr int kSkinnySlices = 2;           // k slices in flight per wave (registers)
 
-template <bool B_TR>
-__global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_skinny_kernel(TunedGemmArgs a) {
+template <bool B_TR, typename E>
+__global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_skinny_kernel(TunedGemmArgs a, E e) {
   constexpr int NW = kSkinnyWaves, SL = kSkinnySlices;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -425,6 +463,18 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_skinny_kernel(Tun
   f32x4 sum = red[tid];
 #pragma unroll
   for (int w = 1; w < NW; ++w) sum += red[w * 256 + tid];
+  if constexpr (kLinear<E>) {   // four waves: pieces of eight columns, four to a row
+    red[tid] = sum;             // (its own place)
+    __syncthreads();
+    if (tid >= 128) return;
+    const int row = tid >> 2, vq = tid & 3;
+    const f32x4 lo4 = red[vq * 64 + row], hi4 = red[vq * 64 + 32 + row];
+    float v[8] = {lo4[0], lo4[1], lo4[2], lo4[3], hi4[0], hi4[1], hi4[2], hi4[3]}, res[8];
+    EpilogueColumns<uint16_t> ec(e, n0 + 8 * vq);
+    ec.residual(m0 + row, e, res);
+    ec.finish(v, m0 + row, res, e, drop_key(e.drop));
+    return;
+  }
   const int64_t m = m0 + (tid & 31), n = n0 + 8 * (tid >> 6) + 4 * ((tid >> 5) & 1);
   if (m < a.M) {
     u32x2 pk;
@@ -434,13 +484,13 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_skinny_kernel(Tun
   }
 }
 
-template <bool B_TR>
-int launch_skinny(const TunedGemmArgs& a, hipStream_t stream) {
-  if (hipError_t e0 = LdsLimit<&gemm_bf16_skinny_kernel<B_TR>, kSkinnyLds>::ensure(); e0 != hipSuccess)
+template <bool B_TR, typename E>
+int launch_skinny(const TunedGemmArgs& a, const E& e, hipStream_t stream) {
+  if (hipError_t e0 = LdsLimit<&gemm_bf16_skinny_kernel<B_TR, E>, kSkinnyLds>::ensure(); e0 != hipSuccess)
     return (int)e0;
-  hipLaunchKernelGGL(gemm_bf16_skinny_kernel<B_TR>,
+  hipLaunchKernelGGL((gemm_bf16_skinny_kernel<B_TR, E>),
                      dim3((unsigned)(a.N / kSkinnyCols), (unsigned)((a.M + kSkinnyRows - 1) / kSkinnyRows)),
-                     dim3(64 * kSkinnyWaves), kSkinnyLds, stream, a);
+                     dim3(64 * kSkinnyWaves), kSkinnyLds, stream, a, e);
   return (int)hipGetLastError();
 }
 
@@ -459,8 +509,8 @@ int launch_skinny(const TunedGemmArgs& a, hipStream_t stream) {
 constexpr int kFewCols = 16, kFewTile = 1024;   // LDS of one product's transposed weights
 // rows up to which it is the faster one, by the weights' form
 bool few_takes(bool b_tr, int64_t M) { return M <= (b_tr ? 16 : 8); }
-template <bool B_TR>
-__global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_few_kernel(TunedGemmArgs a) {
+template <bool B_TR, typename E>
+__global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_few_kernel(TunedGemmArgs a, E e) {
   constexpr int NW = kSkinnyWaves, SL = kSkinnySlices;
   __shared__ __attribute__((aligned(16))) unsigned char smem[NW * SL * 2 * kFewTile];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -514,14 +564,27 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_few_kernel(TunedG
   f32x4 sum = red[lane];
 #pragma unroll
   for (int w = 1; w < NW; ++w) sum += red[w * 64 + lane];
+  if constexpr (kLinear<E>) {   // one wave: pieces of eight columns, two to a row
+    red[lane] = sum;
+    __builtin_amdgcn_wave_barrier();
+    if (lane >= 32) return;
+    const int row = lane >> 1, q = lane & 1;
+    const f32x4 lo4 = red[32 * q + row], hi4 = red[32 * q + 16 + row];
+    float v[8] = {lo4[0], lo4[1], lo4[2], lo4[3], hi4[0], hi4[1], hi4[2], hi4[3]}, res[8];
+    EpilogueColumns<uint16_t> ec(e, n0 + 8 * q);
+    ec.residual(row, e, res);
+    ec.finish(v, row, res, e, drop_key(e.drop));
+    return;
+  }
   if (i16 < a.M)
     *reinterpret_cast<u32x2*>(a.C + i16 * a.ldc + n0 + 4 * gq) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
 }
 
-template <bool B_TR>
-int launch_few(TunedGemmArgs a, hipStream_t stream) {
+template <bool B_TR, typename E>
+int launch_few(TunedGemmArgs a, const E& e, hipStream_t stream) {
   a.n_items = a.N / kFewCols;
-  hipLaunchKernelGGL(gemm_bf16_few_kernel<B_TR>, dim3((unsigned)xcd_grid_size(a.n_items)), dim3(64 * kSkinnyWaves), 0, stream, a);
+  hipLaunchKernelGGL((gemm_bf16_few_kernel<B_TR, E>), dim3((unsigned)xcd_grid_size(a.n_items)), dim3(64 * kSkinnyWaves),
+                     0, stream, a, e);
   return (int)hipGetLastError();
 }
 
@@ -550,30 +613,42 @@ GemmPlan plan_tiles(bool a_tr, int64_t M, int64_t N, int64_t K) {
   return best;
 }
 
-template <bool A_TR, bool B_TR, typename G>
-int launch_shape(TunedGemmArgs a, hipStream_t stream) {
+template <bool A_TR, bool B_TR, typename G, typename E>
+int launch_shape(TunedGemmArgs a, const E& e, hipStream_t stream) {
   a.tiles_n = (a.N + G::BN - 1) / G::BN;
   a.n_items = ((a.M + G::BM - 1) / G::BM) * a.tiles_n * a.splits;
-  if (hipError_t e0 = LdsLimit<&gemm_bf16_kernel<A_TR, B_TR, G>, G::kLds>::ensure(); e0 != hipSuccess) return (int)e0;
-  hipLaunchKernelGGL((gemm_bf16_kernel<A_TR, B_TR, G>), dim3((unsigned)xcd_grid_size(a.n_items)), dim3(64 * G::NW),
-                     G::kLds, stream, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.splits == 1 || !a.C) return (int)e;
+  if (hipError_t e0 = LdsLimit<&gemm_bf16_kernel<A_TR, B_TR, G, E>, G::kLds>::ensure(); e0 != hipSuccess) return (int)e0;
+  hipLaunchKernelGGL((gemm_bf16_kernel<A_TR, B_TR, G, E>), dim3((unsigned)xcd_grid_size(a.n_items)), dim3(64 * G::NW),
+                     G::kLds, stream, a, e);
+  const hipError_t rc = hipGetLastError();
+  if (rc != hipSuccess || a.splits == 1 || !a.C) return (int)rc;
   const int64_t n4 = a.M * a.N / 4;
   hipLaunchKernelGGL(gemm_bf16_reduce_kernel, dim3((unsigned)((n4 + 255) / 256)), dim3(256), 0,
                      stream, a);
   return (int)hipGetLastError();
 }
-template <bool A_TR, bool B_TR>
-int launch_form(const TunedGemmArgs& a, int shape, hipStream_t stream) {
+template <bool A_TR, bool B_TR, typename E>
+int launch_form(const TunedGemmArgs& a, const E& e, int shape, hipStream_t stream) {
   switch (shape) {
-    case 0: return launch_shape<A_TR, B_TR, Tile256x256>(a, stream);
-    case 1: return launch_shape<A_TR, B_TR, Tile256x128>(a, stream);
-    case 2: return launch_shape<A_TR, B_TR, Tile128x128>(a, stream);
+    case 0: return launch_shape<A_TR, B_TR, Tile256x256>(a, e, stream);
+    case 1: return launch_shape<A_TR, B_TR, Tile256x128>(a, e, stream);
+    case 2: return launch_shape<A_TR, B_TR, Tile128x128>(a, e, stream);
     default: break;
   }
   if constexpr (A_TR) return -1;
-  else return launch_shape<A_TR, B_TR, Tile64x128>(a, stream);
+  else return launch_shape<A_TR, B_TR, Tile64x128>(a, e, stream);
+}
+template <typename E>
+int launch_tiles(bool a_tr, bool b_tr, const TunedGemmArgs& a, const E& e, int shape, hipStream_t stream) {
+  if (!a_tr && b_tr) return launch_form<false, true>(a, e, shape, stream);
+  if (!a_tr && !b_tr) return launch_form<false, false>(a, e, shape, stream);
+  if (a_tr && b_tr) return launch_form<true, true>(a, e, shape, stream);
+  return -1;   // transposed A with row-form B: no caller
+}
+template <typename E>
+int launch_few_rows(bool b_tr, const TunedGemmArgs& a, const E& e, hipStream_t stream) {
+  if (few_takes(b_tr, a.M)) return b_tr ? launch_few<true>(a, e, stream) : launch_few<false>(a, e, stream);
+  return b_tr ? launch_skinny<true>(a, e, stream) : launch_skinny<false>(a, e, stream);
 }
 
 }  // namespace
@@ -640,31 +715,33 @@ int launch_gemm_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const voi
   a.slices_per_split = plan.slices_per_split;
   a.P = plan.splits > 1 ? static_cast<float*>(ws) : nullptr;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (!a_tr && skinny_takes(M, N, K) && !accumulate) {
-    if (few_takes(b_tr, M)) return b_tr ? launch_few<true>(a, st) : launch_few<false>(a, st);
-    return b_tr ? launch_skinny<true>(a, st) : launch_skinny<false>(a, st);
-  }
+  if (!a_tr && skinny_takes(M, N, K) && !accumulate) return launch_few_rows(b_tr, a, NoEpilogue{}, st);
   if (a.splits > 1 && !ws) return -1;
-  if (!a_tr && b_tr) return launch_form<false, true>(a, plan.shape, st);
-  if (!a_tr && !b_tr) return launch_form<false, false>(a, plan.shape, st);
-  if (a_tr && b_tr) return launch_form<true, true>(a, plan.shape, st);
-  return -1;   // transposed A with row-form B: no caller
+  return launch_tiles(a_tr, b_tr, a, NoEpilogue{}, plan.shape, st);
 }
 
-int launch_gemm_bf16_partials(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb,
-                              float* P, int64_t M, int64_t N, int64_t K, int* splits, void* stream) {
+size_t linear_bf16_workspace_bytes(bool a_tr, int64_t M, int64_t N, int64_t K) {
+  if (!a_tr && skinny_takes(M, N, K)) return 0;
+  const int splits = plan_tiles(a_tr, M, N, K).splits;
+  return splits > 1 ? (size_t)splits * M * N * sizeof(float) : 0;
+}
+
+int launch_linear_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M,
+                       int64_t N, int64_t K, const Epilogue& e0, void* ws, void* stream) {
+  const Epilogue e = with_vec(e0, 1);
   const GemmPlan plan = plan_tiles(a_tr, M, N, K);
   TunedGemmArgs a = {};
   a.A = static_cast<const uint16_t*>(A);
   a.B = static_cast<const uint16_t*>(B);
   a.M = M; a.N = N; a.K = K; a.lda = lda; a.ldb = ldb;
-  a.splits = *splits = plan.splits;
+  a.splits = plan.splits;
   a.slices_per_split = plan.slices_per_split;
-  a.P = P;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (!a_tr && b_tr) return launch_form<false, true>(a, plan.shape, st);
-  if (!a_tr && !b_tr) return launch_form<false, false>(a, plan.shape, st);
-  return a_tr && b_tr ? launch_form<true, true>(a, plan.shape, st) : -1;
+  if (!a_tr && skinny_takes(M, N, K)) return launch_few_rows(b_tr, a, e, st);
+  if (a.splits == 1) return launch_tiles(a_tr, b_tr, a, e, plan.shape, st);
+  a.P = static_cast<float*>(ws);
+  const int rc = launch_tiles(a_tr, b_tr, a, NoEpilogue{}, plan.shape, st);
+  return rc ? rc : launch_linear_epilogue(1, {a.P, N, a.splits}, e, stream);
 }
 
 }  // namespace mhffn

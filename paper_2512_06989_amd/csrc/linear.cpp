@@ -39,21 +39,16 @@ struct Operands {
   int64_t ldz(const Linear& p) const { return p.dtype == 1 ? Np : p.N; }
 };
 
-size_t partial_bytes(int dtype, int64_t M, int64_t N, int64_t K) {
-  const size_t one = (size_t)M * N * 4, all = dtype == 1 ? gemm_bf16_workspace_bytes(M, N, K) : 0;
-  return all > one ? all : one;
+size_t partial_bytes(int dtype, bool a_tr, int64_t M, int64_t N, int64_t K) {
+  return dtype == 1 ? linear_bf16_workspace_bytes(a_tr, M, N, K) : (size_t)M * N * 4;
 }
 
-// C (epilogue e) = A B over the partial products of the tuned kernel, N padded to eight
+// Epilogue e over A B
 int product(int dtype, bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M,
             int64_t N, int64_t K, float* P, const Epilogue& e, void* stream) {
-  LinearSums s = {P, N, 1};
-  int rc;
-  if (dtype == 1)
-    rc = launch_gemm_bf16_partials(a_tr, b_tr, A, lda, B, ldb, P, M, N, K, &s.splits, stream);
-  else
-    rc = launch_gemm(0, A, a_tr ? 1 : lda, a_tr ? lda : 1, B, b_tr ? 1 : ldb, b_tr ? ldb : 1, P, N, M, N, K, stream);
-  return rc ? rc : launch_linear_epilogue(dtype, s, e, stream);
+  if (dtype == 1) return launch_linear_bf16(a_tr, b_tr, A, lda, B, ldb, M, N, K, e, P, stream);
+  const int rc = launch_gemm(0, A, a_tr ? 1 : lda, a_tr ? lda : 1, B, b_tr ? 1 : ldb, b_tr ? ldb : 1, P, N, M, N, K, stream);
+  return rc ? rc : launch_linear_epilogue(dtype, {P, N, 1}, e, stream);
 }
 
 Epilogue plain(void* Y, int64_t ldy, int64_t M, int64_t N) {
@@ -70,7 +65,7 @@ int forward(const Linear& p, const void* X, const void* W, const void* bias, con
   void* const Xp = o.x ? arena.take((size_t)p.M * o.Kp * 2) : nullptr;
   void* const Wp = o.w ? arena.take((size_t)o.Kp * o.Np * 2) : nullptr;
   const int64_t K = o.x || o.w ? o.Kp : p.K, N = bf16 ? up(p.N, 8) : p.N;
-  float* const P = static_cast<float*>(arena.take(partial_bytes(p.dtype, p.M, N, K)));
+  float* const P = static_cast<float*>(arena.take(partial_bytes(p.dtype, false, p.M, N, K)));
   if (bytes) {
     *bytes = arena.used;
     return 0;
@@ -100,7 +95,7 @@ int backward(const Linear& p, const void* X, const void* W, const void* Z, const
   const int64_t Nk = bf16 ? o.Np : p.N;   // the contraction of dX
   void* const dZ = o.dz ? arena.take((size_t)p.M * ldz * elt(p.dtype)) : nullptr;
   float* const sums = static_cast<float*>(arena.take((size_t)linear_column_blocks(p.M, p.N) * p.N * 4));
-  const size_t px = partial_bytes(p.dtype, p.M, K8, Nk), pw = partial_bytes(p.dtype, K8, N8, p.M);
+  const size_t px = partial_bytes(p.dtype, false, p.M, K8, Nk), pw = partial_bytes(p.dtype, true, K8, N8, p.M);
   float* const P = static_cast<float*>(arena.take(px > pw ? px : pw));
   if (bytes) {
     *bytes = arena.used;

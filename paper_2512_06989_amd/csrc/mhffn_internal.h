@@ -101,11 +101,6 @@ size_t gemm_bf16_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int launch_gemm_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb,
                      void* C, int64_t ldc, int64_t M, int64_t N, int64_t K, void* ws, void* stream,
                      bool accumulate = false);
-// The same product as its fp32 partial sums alone, P [splits][M][N]; returns their number in
-// *splits (at most gemm_bf16_workspace_bytes() / (4 M N), 1 where that is 0).
-int launch_gemm_bf16_partials(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb,
-                              float* P, int64_t M, int64_t N, int64_t K, int* splits, void* stream);
-
 // ---- linear layer with its epilogue, dropout ---------------------------------
 // Dropout after validation: an element stays where its 16 random bits reach `threshold`
 // (0: all stay, the generator is not read; 65536: none does).
@@ -146,6 +141,12 @@ struct LinearSums {   // Epilogue over `splits` partial products P [splits][M][l
   int64_t ldp;
   int splits;
 };
+// The product of the forms that launch_gemm_bf16 takes, followed by the epilogue: in the product's
+// kernel where it is not split, over its partial sums in `ws` otherwise.  N % 8 == 0 (e.N of the
+// columns exist); row-form operands hold K % 32 == 0.
+size_t linear_bf16_workspace_bytes(bool a_tr, int64_t M, int64_t N, int64_t K);
+int launch_linear_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb,
+                       int64_t M, int64_t N, int64_t K, const Epilogue& e, void* ws, void* stream);
 int launch_linear_epilogue(int dtype, const LinearSums& s, const Epilogue& e, void* stream);
 // [rows][cols] (row stride ld) -> dense [rows_to][cols_to], zero outside
 int launch_pack(int dtype, const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst,

@@ -130,15 +130,6 @@ __global__ __launch_bounds__(kThreads) void column_sum_kernel(const float* parti
   else out[c] = sum;
 }
 
-inline bool vec_rows(const void* p, int64_t ld, int dtype) {
-  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % (dtype == 1 ? 8 : 4) == 0;
-}
-Epilogue with_vec(Epilogue e, int dtype) {
-  e.vec = (vec_rows(e.Z, e.ldz, dtype) ? 1 : 0) | (vec_rows(e.residual, e.ldr, dtype) ? 2 : 0) |
-          (vec_rows(e.Y, e.ldy, dtype) ? 4 : 0);
-  return e;
-}
-
 DzGrid dz_grid(int64_t M, int64_t N, int64_t cols_to) {
   DzGrid g;
   g.pieces = ((cols_to > N ? cols_to : N) + 7) / 8;
