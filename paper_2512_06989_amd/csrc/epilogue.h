@@ -62,44 +62,71 @@ __device__ __forceinline__ void drop8(float (&v)[8], uint64_t piece, const Dropo
 }
 
 // ---- activations (ACT: mhffn_activation) --------------------------------------------------------
-template <int ACT>
+// Phi(-|z|) and exp(-z^2 / 2) for bf16 results: Abramowitz and Stegun, Handbook of Mathematical
+// Functions, 7.1.26, good to 1.5e-7 absolute, with the one exponential that the slope needs too.
+// |z| stops at 30, where both are 0 in fp32, so that infinities give the limits.
+struct NormalTail { float a, q, e; };
+__device__ __forceinline__ NormalTail normal_tail(float z) {
+  NormalTail n;
+  n.a = fminf(fabsf(z), 30.f);
+  n.e = __builtin_amdgcn_exp2f(-0.5f * MHFFN_LOG2E * n.a * n.a);
+  const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * 0.70710678118654752f * n.a);
+  float p = 0.5f * 1.061405429f;
+  p = p * t - 0.5f * 1.453152027f;
+  p = p * t + 0.5f * 1.421413741f;
+  p = p * t - 0.5f * 0.284496736f;
+  p = p * t + 0.5f * 0.254829592f;
+  n.q = p * t * n.e;
+  return n;
+}
+// NaN stays NaN in each.  Results of type T: fp32 takes the library's erf (its products are sixteen
+// times as long), bf16 the tail above: 40 instructions an element against 16.
+template <int ACT, typename T>
 __device__ __forceinline__ float activate(float z) {
-  if constexpr (ACT == 1) return z < 0.f ? 0.f : z;              // (NaN stays NaN)
+  if constexpr (ACT == 1) return z < 0.f ? 0.f : z;
   else if constexpr (ACT == 2) return z * sigmoid_fast(z);
-  else if constexpr (ACT == 3) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-  else return z;
+  else if constexpr (ACT == 3 && sizeof(T) == 4) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+  else if constexpr (ACT == 3) {
+    const NormalTail n = normal_tail(z);
+    return (z < 0.f ? 0.f : z) - n.a * n.q;   // z Phi(z)
+  } else return z;
 }
 // act'(z)
-template <int ACT>
+template <int ACT, typename T>
 __device__ __forceinline__ float slope(float z) {
   if constexpr (ACT == 1) return z <= 0.f ? 0.f : 1.f;
   else if constexpr (ACT == 2) {
     const float s = sigmoid_fast(z);
     return s + z * s * (1.f - s);
-  } else if constexpr (ACT == 3) {
+  } else if constexpr (ACT == 3 && sizeof(T) == 4) {
     return 0.5f * (1.f + erff(z * 0.70710678118654752f)) +
            z * (0.39894228040143268f * __builtin_amdgcn_exp2f(-0.5f * MHFFN_LOG2E * z * z));
+  } else if constexpr (ACT == 3) {
+    const NormalTail n = normal_tail(z);
+    return (z < 0.f ? n.q : 1.f - n.q) + z * (0.39894228040143268f * n.e);
   } else return 1.f;
 }
-template <int ACT>
+template <int ACT, typename T>
 __device__ __forceinline__ void activate8(float (&v)[8]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = activate<ACT>(v[j]);
+  for (int j = 0; j < 8; ++j) v[j] = activate<ACT, T>(v[j]);
 }
+template <typename T>
 __device__ __forceinline__ void activate8(float (&v)[8], int act) {
-  if (act == 1) activate8<1>(v);
-  else if (act == 2) activate8<2>(v);
-  else if (act == 3) activate8<3>(v);
+  if (act == 1) activate8<1, T>(v);
+  else if (act == 2) activate8<2, T>(v);
+  else if (act == 3) activate8<3, T>(v);
 }
-template <int ACT>
+template <int ACT, typename T>
 __device__ __forceinline__ void slope8(float (&v)[8], const float (&z)[8]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] *= slope<ACT>(z[j]);
+  for (int j = 0; j < 8; ++j) v[j] *= slope<ACT, T>(z[j]);
 }
+template <typename T>
 __device__ __forceinline__ void slope8(float (&v)[8], const float (&z)[8], int act) {
-  if (act == 1) slope8<1>(v, z);
-  else if (act == 2) slope8<2>(v, z);
-  else if (act == 3) slope8<3>(v, z);
+  if (act == 1) slope8<1, T>(v, z);
+  else if (act == 2) slope8<2, T>(v, z);
+  else if (act == 3) slope8<3, T>(v, z);
 }
 
 // ---- pieces of eight columns in memory -----------------------------------------------------------
@@ -177,7 +204,7 @@ struct EpilogueColumns {
       for (int j = 0; j < 8; ++j) v[j] += bias[j];
     }
     if (e.Z) store8(static_cast<T*>(e.Z) + row * e.ldz + col, cols, e.vec & 1, v);
-    activate8(v, e.act);
+    activate8<T>(v, e.act);
     drop8(v, (uint64_t)row * (uint64_t)((e.N + 7) >> 3) + (uint64_t)(col >> 3), e.drop, key);
     if (e.residual) {
 #pragma unroll
@@ -192,6 +219,43 @@ __device__ __forceinline__ void epilogue8(float (&v)[8], int64_t row, int64_t co
   float r[8];
   ec.residual(row, e, r);
   ec.finish(v, row, r, e, key);
+}
+
+// A wave's piece of a product (32 IM rows m, 32 IN columns n, n on the matrix row axis: lane (r, g) holds columns
+// 32 jn + 8 vq + 4 g + i of row 32 im + r in register 4 vq + i of acc[jn][im]).  The sums pass through LDS in
+// fp32, 32 rows at a time (`piece`, the wave's own 32 x 32 IN floats; the 16-byte chunks of a row are permuted by the
+// row), so that a lane holds eight columns of one row: whole rows of the residual, Z and Y move, and a call
+// of the generator serves the lane that makes it.
+template <typename T, int IM, int IN>
+__device__ __forceinline__ void wave_epilogue(const f32x16 (&acc)[IN][IM], unsigned char* piece, int64_t m, int64_t n,
+                                              int lane, const Epilogue& e) {
+  constexpr int CH = 8 * IN, LPR = 4 * IN, RPP = 64 / LPR, PASSES = 32 / RPP, ROW = 128 * IN;
+  const DropKey key = drop_key(e.drop);
+  const int r = lane & 31, g = lane >> 5, lrow = lane / LPR, c = 2 * (lane % LPR);
+  const EpilogueColumns<T> ec(e, n + 8 * (lane % LPR));
+#pragma unroll
+  for (int im = 0; im < IM; ++im) {
+    const int64_t mb = m + 32 * im;
+    float res[PASSES][8];
+#pragma unroll
+    for (int q = 0; q < PASSES; ++q) ec.residual(mb + q * RPP + lrow, e, res[q]);
+#pragma unroll
+    for (int jn = 0; jn < IN; ++jn)
+#pragma unroll
+      for (int vq = 0; vq < 4; ++vq)
+        *reinterpret_cast<f32x4*>(piece + r * ROW + (((8 * jn + 2 * vq + g) ^ (r & (CH - 1))) << 4)) =
+            f32x4{acc[jn][im][4 * vq], acc[jn][im][4 * vq + 1], acc[jn][im][4 * vq + 2], acc[jn][im][4 * vq + 3]};
+    __builtin_amdgcn_wave_barrier();   // (one wave: its reads follow its writes in the same queue)
+#pragma unroll
+    for (int q = 0; q < PASSES; ++q) {
+      const int row = q * RPP + lrow;
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(piece + row * ROW + ((c ^ (row & (CH - 1))) << 4));
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(piece + row * ROW + (((c + 1) ^ (row & (CH - 1))) << 4));
+      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      ec.finish(v, mb + row, res[q], e, key);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
 }
 
 // Host: which row tensors move whole pieces

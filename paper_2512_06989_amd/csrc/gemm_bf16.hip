@@ -257,38 +257,8 @@ __global__ __launch_bounds__(64 * G::NW, G::BM == 256 ? 2 : 4) void gemm_bf16_ke
 
   // ---- store: lane = row m, registers = four consecutive n per group ----------------------
   if constexpr (kLinear<E>) {
-    // The sums pass through LDS in fp32, 32 rows of the wave's piece at a time (16-byte chunks of a
-    // row permuted by the row), so that a lane holds eight columns of one row: whole rows of the
-    // residual, Z and Y move, and a call of the generator serves the lane that makes it.
-    constexpr int CH = G::TN / 4, LPR = G::TN / 8, RPP = 64 / LPR, PASSES = 32 / RPP;
-    const DropKey key = drop_key(e.drop);
     __syncthreads();                                   // the stages are done with
-    unsigned char* piece = smem + wave * (32 * G::TN * 4);
-    const int64_t n = n0 + G::TN * wn + 8 * (lane % LPR);
-    EpilogueColumns<uint16_t> ec(e, n);
-#pragma unroll
-    for (int im = 0; im < IM; ++im) {
-      const int64_t mb = m0 + G::TM * wm + 32 * im;
-      float res[PASSES][8];
-#pragma unroll
-      for (int q = 0; q < PASSES; ++q) ec.residual(mb + q * RPP + lane / LPR, e, res[q]);
-#pragma unroll
-      for (int jn = 0; jn < IN; ++jn)
-#pragma unroll
-        for (int vq = 0; vq < 4; ++vq)
-          *reinterpret_cast<f32x4*>(piece + r * (G::TN * 4) + (((8 * jn + 2 * vq + g) ^ (r & (CH - 1))) << 4)) =
-              f32x4{acc[jn][im][4 * vq], acc[jn][im][4 * vq + 1], acc[jn][im][4 * vq + 2], acc[jn][im][4 * vq + 3]};
-      __builtin_amdgcn_wave_barrier();                 // (the piece is this wave's own: one queue)
-#pragma unroll
-      for (int q = 0; q < PASSES; ++q) {
-        const int row = q * RPP + lane / LPR, c = 2 * (lane % LPR);
-        const f32x4 lo4 = *reinterpret_cast<const f32x4*>(piece + row * (G::TN * 4) + ((c ^ (row & (CH - 1))) << 4));
-        const f32x4 hi4 = *reinterpret_cast<const f32x4*>(piece + row * (G::TN * 4) + (((c + 1) ^ (row & (CH - 1))) << 4));
-        float v[8] = {lo4[0], lo4[1], lo4[2], lo4[3], hi4[0], hi4[1], hi4[2], hi4[3]};
-        ec.finish(v, mb + row, res[q], e, key);
-      }
-      __builtin_amdgcn_wave_barrier();
-    }
+    wave_epilogue<uint16_t, IM, IN>(acc, smem + wave * (32 * G::TN * 4), m0 + G::TM * wm, n0 + G::TN * wn, lane, e);
     return;
   }
   if (a.P || a.accumulate) {

@@ -1,0 +1,209 @@
+// fp32 product of the linear layer, C[m][n] = sum_k A(m,k) B(n,k), with its epilogue.  The forms are
+// those of the bf16 product: an operand lies with k contiguous ("row form") or with its row index
+// contiguous ("transposed form").  Any sizes, any strides.
+//
+// What bounds it: the fp32 matrix rate, 256 flop per clock and CU, a sixteenth of bf16's.  A slice of 32
+// k of a 128 x 128 tile is 4096 clocks of products against 32 KB to load and 64 KB of operands to
+// read from LDS, so loads go through registers (zeros past every edge, no alignment asked for), LDS
+// holds two slices, and one barrier separates them.
+// v_mfma_f32_32x32x2_f32: lane (r, g) holds row r (column r), k = g.  Step s of eight k takes k = 4 g + s of
+// both operands, so that a lane of a row-form operand reads its four steps at once.  n is on the
+// matrix row axis: a lane ends up with four consecutive n of one row m, as in the bf16 product.
+// LDS: row form [rows][32 + 4], transposed form [32 k][rows + 8] (the two halves of a wave, four k apart, lie 32
+// banks apart): no bank conflicts in either.
+#include "epilogue.h"
+
+#include <type_traits>
+
+namespace mhffn {
+namespace {
+
+constexpr int kFK = 32, kFThreads = 256;
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+struct GemmF32Args {
+  const float* A;      // m side
+  const float* B;      // n side
+  int64_t M, N, K, lda, ldb;
+  int64_t tiles_n, n_items;
+  int splits;
+  int64_t k_per_split; // a multiple of kFK
+};
+
+template <bool TR, int ROWS>
+struct OperandF32 {
+  static constexpr int kLd = TR ? ROWS + 8 : kFK + 4;
+  static constexpr int kFloats = TR ? kFK * kLd : ROWS * kLd;
+  static constexpr int kVecs = ROWS * kFK / 4 / kFThreads;   // 16-byte pieces per thread and slice
+  // piece q of a thread: (row, k) of its first element
+  static __device__ __forceinline__ void place(int q, int tid, int& row, int& k) {
+    const int i = q * kFThreads + tid;
+    if constexpr (TR) { k = i / (ROWS / 4); row = i % (ROWS / 4) * 4; }
+    else { row = i / (kFK / 4); k = i % (kFK / 4) * 4; }
+  }
+  // src: element (row 0 of the tile, k 0 of the slice); rows, ks: how many of each exist
+  static __device__ __forceinline__ void load(const float* src, int64_t ld, int64_t rows, int64_t ks, int tid, f32x4 (&v)[kVecs]) {
+    const bool whole = rows >= ROWS && ks >= kFK;
+#pragma unroll
+    for (int q = 0; q < kVecs; ++q) {
+      int row, k;
+      place(q, tid, row, k);
+      const float* p = TR ? src + k * ld + row : src + row * ld + k;
+      if (whole || (TR ? k < ks && row + 4 <= rows : row < rows && k + 4 <= ks)) {
+        v[q] = *reinterpret_cast<const f32x4_any*>(p);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[q][j] = (TR ? k < ks && row + j < rows : row < rows && k + j < ks) ? p[j] : 0.f;
+      }
+    }
+  }
+  static __device__ __forceinline__ void store(float* lds, int tid, const f32x4 (&v)[kVecs]) {
+#pragma unroll
+    for (int q = 0; q < kVecs; ++q) {
+      int row, k;
+      place(q, tid, row, k);
+      *reinterpret_cast<f32x4*>(lds + (TR ? k * kLd + row : row * kLd + k)) = v[q];
+    }
+  }
+  // the four steps of k = 8 j .. 8 j + 7 of row `row`
+  static __device__ __forceinline__ f32x4 read(const float* lds, int row, int j, int g) {
+    if constexpr (TR) {
+      f32x4 v;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) v[s] = lds[(8 * j + 4 * g + s) * kLd + row];
+      return v;
+    } else {
+      return *reinterpret_cast<const f32x4*>(lds + row * kLd + 8 * j + 4 * g);
+    }
+  }
+};
+
+template <bool A_TR, bool B_TR, int TILE>
+__global__ __launch_bounds__(kFThreads, 2) void gemm_f32_kernel(GemmF32Args a, Epilogue e) {
+  constexpr int W = TILE / 2, I = W / 32;     // four waves of W x W
+  using OA = OperandF32<A_TR, TILE>;
+  using OB = OperandF32<B_TR, TILE>;
+  constexpr int kStage = OA::kFloats + OB::kFloats;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  float* const lds = reinterpret_cast<float*>(smem);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, g = lane >> 5;
+  const int64_t item = xcd_work_item(blockIdx.x, a.n_items);
+  if (item >= a.n_items) return;
+  const int split = (int)(item % a.splits);
+  const int64_t tile = item / a.splits, m0 = tile / a.tiles_n * TILE, n0 = tile % a.tiles_n * TILE;
+  const int64_t k0 = split * a.k_per_split, k1 = k0 + a.k_per_split < a.K ? k0 + a.k_per_split : a.K;
+  const int wm = (wave >> 1) * W, wn = (wave & 1) * W;
+
+  f32x16 acc[I][I];
+#pragma unroll
+  for (int i = 0; i < I; ++i)
+#pragma unroll
+    for (int j = 0; j < I; ++j) acc[i][j] = f32x16{0};
+
+  f32x4 va[OA::kVecs], vb[OB::kVecs];
+  const float* const pa = a.A + (A_TR ? m0 : m0 * a.lda);
+  const float* const pb = a.B + (B_TR ? n0 : n0 * a.ldb);
+  auto load = [&](int64_t k) {
+    OA::load(pa + (A_TR ? k * a.lda : k), a.lda, a.M - m0, k1 - k, tid, va);
+    OB::load(pb + (B_TR ? k * a.ldb : k), a.ldb, a.N - n0, k1 - k, tid, vb);
+  };
+  auto store = [&](int stage) {
+    OA::store(lds + stage * kStage, tid, va);
+    OB::store(lds + stage * kStage + OA::kFloats, tid, vb);
+  };
+  load(k0);
+  store(0);
+  __syncthreads();
+  int stage = 0;
+  for (int64_t k = k0; k < k1; k += kFK) {
+    if (k + kFK < k1) load(k + kFK);
+    const float* const la = lds + stage * kStage;
+    const float* const lb = la + OA::kFloats;
+#pragma unroll
+    for (int j = 0; j < kFK / 8; ++j) {
+      f32x4 fa[I], fb[I];
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+        fa[i] = OA::read(la, wm + 32 * i + r, j, g);
+        fb[i] = OB::read(lb, wn + 32 * i + r, j, g);
+      }
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+          for (int n = 0; n < I; ++n) acc[n][i] = __builtin_amdgcn_mfma_f32_32x32x2f32(fb[n][s], fa[i][s], acc[n][i], 0, 0, 0);
+    }
+    stage ^= 1;
+    if (k + kFK < k1) store(stage);
+    __syncthreads();   // (everyone has read the slice that the next store overwrites)
+  }
+  if (a.splits > 1) e.Y = static_cast<float*>(e.Y) + (int64_t)split * a.M * a.N;   // partial sums (16-byte aligned rows: N % 4 == 0)
+  wave_epilogue<float, I, I>(acc, smem + wave * (32 * W * 4), m0 + wm, n0 + wn, lane, e);
+}
+
+// Tile and split of the contraction: the workgroups of a CU share its matrix rate, so the time is
+// that of the fullest CU; clocks of a CU, measured around them 3000 a workgroup, and for the sum
+// over the splits 9000 and 2600 bytes a clock.
+struct F32Plan { int tile, splits; int64_t k_per_split; };
+F32Plan plan_f32(int64_t M, int64_t N, int64_t K) {
+  F32Plan best{128, 1, K};
+  double least = 0.0;
+  for (int tile : {128, 64}) {
+    const int64_t tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile);
+    for (int want = 1; want <= 16; ++want) {
+      const int64_t per = ((K + want - 1) / want + kFK - 1) / kFK * kFK;
+      if (want > 1 && (per < 2 * kFK || (K + per - 1) / per != want)) continue;
+      const double slice = 2.0 * tile * tile * kFK / 256 * (tile == 128 ? 1.1 : 1.25);
+      double cost = (double)((tiles * want + 255) / 256) * ((double)((per + kFK - 1) / kFK) * slice + 3000);
+      if (want > 1) cost += 9000 + (double)want * M * N * 4 / 2600;
+      if (least == 0.0 || cost < least) { least = cost; best = {tile, want, per}; }
+    }
+  }
+  return best;
+}
+
+template <bool A_TR, bool B_TR, int TILE>
+int launch_tile(GemmF32Args a, const Epilogue& e, hipStream_t stream) {
+  constexpr int kStages = 2 * (OperandF32<A_TR, TILE>::kFloats + OperandF32<B_TR, TILE>::kFloats) * 4;
+  constexpr int kOut = 4 * 32 * (TILE / 2) * 4, kLds = kStages > kOut ? kStages : kOut;
+  a.tiles_n = (a.N + TILE - 1) / TILE;
+  a.n_items = (a.M + TILE - 1) / TILE * a.tiles_n * a.splits;
+  if (hipError_t e0 = LdsLimit<&gemm_f32_kernel<A_TR, B_TR, TILE>, kLds>::ensure(); e0 != hipSuccess) return (int)e0;
+  hipLaunchKernelGGL((gemm_f32_kernel<A_TR, B_TR, TILE>), dim3((unsigned)xcd_grid_size(a.n_items)), dim3(kFThreads), kLds,
+                     stream, a, e);
+  return (int)hipGetLastError();
+}
+template <int TILE>
+int launch_form(bool a_tr, bool b_tr, const GemmF32Args& a, const Epilogue& e, hipStream_t stream) {
+  if (!a_tr && b_tr) return launch_tile<false, true, TILE>(a, e, stream);
+  if (!a_tr && !b_tr) return launch_tile<false, false, TILE>(a, e, stream);
+  if (a_tr && b_tr) return launch_tile<true, true, TILE>(a, e, stream);
+  return -1;   // transposed A with row-form B: no caller
+}
+
+}  // namespace
+
+size_t linear_f32_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+  const int splits = plan_f32(M, N, K).splits;
+  return splits > 1 ? (size_t)splits * M * N * sizeof(float) : 0;
+}
+
+int launch_linear_f32(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N,
+                      int64_t K, const Epilogue& e0, void* ws, void* stream) {
+  const F32Plan plan = plan_f32(M, N, K);
+  GemmF32Args a = {static_cast<const float*>(A), static_cast<const float*>(B), M, N, K, lda, ldb, 0, 0, plan.splits,
+                   plan.k_per_split};
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Epilogue e = e0;
+  if (plan.splits > 1) {
+    e = {};
+    e.Y = ws; e.ldy = N; e.M = M; e.N = N;
+  }
+  e = with_vec(e, 0);
+  const int rc = plan.tile == 128 ? launch_form<128>(a_tr, b_tr, a, e, st) : launch_form<64>(a_tr, b_tr, a, e, st);
+  if (rc || plan.splits == 1) return rc;
+  return launch_linear_epilogue(0, {static_cast<float*>(ws), N, plan.splits}, e0, stream);
+}
+
+}  // namespace mhffn

@@ -40,15 +40,13 @@ struct Operands {
 };
 
 size_t partial_bytes(int dtype, bool a_tr, int64_t M, int64_t N, int64_t K) {
-  return dtype == 1 ? linear_bf16_workspace_bytes(a_tr, M, N, K) : (size_t)M * N * 4;
+  return dtype == 1 ? linear_bf16_workspace_bytes(a_tr, M, N, K) : linear_f32_workspace_bytes(M, N, K);
 }
 
 // Epilogue e over A B
 int product(int dtype, bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M,
             int64_t N, int64_t K, float* P, const Epilogue& e, void* stream) {
-  if (dtype == 1) return launch_linear_bf16(a_tr, b_tr, A, lda, B, ldb, M, N, K, e, P, stream);
-  const int rc = launch_gemm(0, A, a_tr ? 1 : lda, a_tr ? lda : 1, B, b_tr ? 1 : ldb, b_tr ? ldb : 1, P, N, M, N, K, stream);
-  return rc ? rc : launch_linear_epilogue(dtype, {P, N, 1}, e, stream);
+  return (dtype == 1 ? launch_linear_bf16 : launch_linear_f32)(a_tr, b_tr, A, lda, B, ldb, M, N, K, e, P, stream);
 }
 
 Epilogue plain(void* Y, int64_t ldy, int64_t M, int64_t N) {

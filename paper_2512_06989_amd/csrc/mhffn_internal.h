@@ -147,6 +147,10 @@ struct LinearSums {   // Epilogue over `splits` partial products P [splits][M][l
 size_t linear_bf16_workspace_bytes(bool a_tr, int64_t M, int64_t N, int64_t K);
 int launch_linear_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb,
                        int64_t M, int64_t N, int64_t K, const Epilogue& e, void* ws, void* stream);
+// The same in fp32: any sizes, any strides
+size_t linear_f32_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int launch_linear_f32(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M,
+                      int64_t N, int64_t K, const Epilogue& e, void* ws, void* stream);
 int launch_linear_epilogue(int dtype, const LinearSums& s, const Epilogue& e, void* stream);
 // [rows][cols] (row stride ld) -> dense [rows_to][cols_to], zero outside
 int launch_pack(int dtype, const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst,

@@ -100,7 +100,7 @@ __global__ __launch_bounds__(kThreads) void linear_dz_kernel(LinearDz a, DzGrid 
         if (a.act) {
           float z[8];
           load8(static_cast<const T*>(a.Z) + row * a.N + col, cols, vec & 2, z);
-          slope8(v, z, a.act);
+          slope8<T>(v, z, a.act);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] += v[j];
@@ -120,12 +120,22 @@ __global__ __launch_bounds__(kThreads) void linear_dz_kernel(LinearDz a, DzGrid 
   }
 }
 
+// 32 columns a workgroup: thread (column t % 32, t / 32) adds up every eighth row block, the eight sums meet
+// in LDS (one thread a column waited for each of its loads: 128 row blocks of 1024 columns took 31 us)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void column_sum_kernel(const float* partials, int64_t blocks, int64_t N, T* out) {
-  const int64_t c = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (c >= N) return;
+  __shared__ float sums[kThreads];
+  const int64_t c = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
   float sum = 0.f;
-  for (int64_t b = 0; b < blocks; ++b) sum += partials[b * N + c];
+  if (c < N) {
+#pragma unroll 8
+    for (int64_t b = threadIdx.x >> 5; b < blocks; b += 8) sum += partials[b * N + c];
+  }
+  sums[threadIdx.x] = sum;
+  __syncthreads();
+  if (threadIdx.x >= 32 || c >= N) return;
+#pragma unroll
+  for (int k = 1; k < 8; ++k) sum += sums[32 * k + threadIdx.x];
   if constexpr (sizeof(T) == 2) out[c] = (uint16_t)pack_bf16(sum, 0.f);
   else out[c] = sum;
 }
@@ -195,7 +205,7 @@ int launch_linear_dz(int dtype, const LinearDz& a, void* stream) {
   const int vec = (vec_rows(a.dY, a.ldy, dtype) ? 1 : 0) | (vec_rows(a.Z, a.N, dtype) ? 2 : 0) |
                   (vec_rows(a.dZ, a.ldz, dtype) ? 4 : 0);
   const dim3 grid((unsigned)((g.pieces + (1 << g.lane_shift) - 1) >> g.lane_shift), (unsigned)blocks);
-  const dim3 sum_grid((unsigned)((a.N + kThreads - 1) / kThreads));
+  const dim3 sum_grid((unsigned)((a.N + 31) / 32));
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dtype == 1) hipLaunchKernelGGL(linear_dz_kernel<uint16_t>, grid, dim3(kThreads), 0, st, a, g, vec);
   else hipLaunchKernelGGL(linear_dz_kernel<float>, grid, dim3(kThreads), 0, st, a, g, vec);
