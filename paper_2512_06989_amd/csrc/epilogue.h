@@ -221,17 +221,22 @@ __device__ __forceinline__ void epilogue8(float (&v)[8], int64_t row, int64_t co
   ec.finish(v, row, r, e, key);
 }
 
-// A wave's piece of a product (32 IM rows m, 32 IN columns n, n on the matrix row axis: lane (r, g) holds columns
-// 32 jn + 8 vq + 4 g + i of row 32 im + r in register 4 vq + i of acc[jn][im]).  The sums pass through LDS in
-// fp32, 32 rows at a time (`piece`, the wave's own 32 x 32 IN floats; the 16-byte chunks of a row are permuted by the
-// row), so that a lane holds eight columns of one row: whole rows of the residual, Z and Y move, and a call
-// of the generator serves the lane that makes it.
-template <typename T, int IM, int IN>
-__device__ __forceinline__ void wave_epilogue(const f32x16 (&acc)[IN][IM], unsigned char* piece, int64_t m, int64_t n,
-                                              int lane, const Epilogue& e) {
-  constexpr int CH = 8 * IN, LPR = 4 * IN, RPP = 64 / LPR, PASSES = 32 / RPP, ROW = 128 * IN;
+// A wave's piece of a product, 32 IM rows m by 32 IN columns n.  The sums pass through LDS in fp32, 32 rows at a time
+// (`piece`, the wave's own 32 x 32 IN floats), so that a lane holds eight columns of one row: whole rows of
+// the residual, Z and Y move, and a call of the generator serves the lane that makes it.
+// `put`(im, piece) stores rows 32 im .. + 31 with put_sums: four columns 4 c .. + 3 of a row, the 16-byte
+// chunks of a row permuted by the row (no bank meets two lanes on either side).
+template <int IN>
+__device__ __forceinline__ int sums_off(int row, int c) { return row * (128 * IN) + ((c ^ (row & (8 * IN - 1))) << 4); }
+template <int IN>
+__device__ __forceinline__ void put_sums(unsigned char* piece, int row, int c, f32x4 v) {
+  *reinterpret_cast<f32x4*>(piece + sums_off<IN>(row, c)) = v;
+}
+template <typename T, int IM, int IN, typename Put>
+__device__ __forceinline__ void wave_epilogue_by(Put&& put, unsigned char* piece, int64_t m, int64_t n, int lane, const Epilogue& e) {
+  constexpr int LPR = 4 * IN, RPP = 64 / LPR, PASSES = 32 / RPP;   // lanes per row, rows per pass
   const DropKey key = drop_key(e.drop);
-  const int r = lane & 31, g = lane >> 5, lrow = lane / LPR, c = 2 * (lane % LPR);
+  const int lrow = lane / LPR, c = 2 * (lane % LPR);
   const EpilogueColumns<T> ec(e, n + 8 * (lane % LPR));
 #pragma unroll
   for (int im = 0; im < IM; ++im) {
@@ -239,23 +244,35 @@ __device__ __forceinline__ void wave_epilogue(const f32x16 (&acc)[IN][IM], unsig
     float res[PASSES][8];
 #pragma unroll
     for (int q = 0; q < PASSES; ++q) ec.residual(mb + q * RPP + lrow, e, res[q]);
-#pragma unroll
-    for (int jn = 0; jn < IN; ++jn)
-#pragma unroll
-      for (int vq = 0; vq < 4; ++vq)
-        *reinterpret_cast<f32x4*>(piece + r * ROW + (((8 * jn + 2 * vq + g) ^ (r & (CH - 1))) << 4)) =
-            f32x4{acc[jn][im][4 * vq], acc[jn][im][4 * vq + 1], acc[jn][im][4 * vq + 2], acc[jn][im][4 * vq + 3]};
+    put(im, piece);
     __builtin_amdgcn_wave_barrier();   // (one wave: its reads follow its writes in the same queue)
 #pragma unroll
     for (int q = 0; q < PASSES; ++q) {
       const int row = q * RPP + lrow;
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(piece + row * ROW + ((c ^ (row & (CH - 1))) << 4));
-      const f32x4 hi = *reinterpret_cast<const f32x4*>(piece + row * ROW + (((c + 1) ^ (row & (CH - 1))) << 4));
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(piece + sums_off<IN>(row, c));
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(piece + sums_off<IN>(row, c + 1));
       float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
       ec.finish(v, mb + row, res[q], e, key);
     }
     __builtin_amdgcn_wave_barrier();
   }
+}
+// ... of products of 32 x 32: lane (r, g) holds columns 32 jn + 8 vq + 4 g + i of row 32 im + r in register 4 vq + i
+// of acc[jn][im]
+template <typename T, int IM, int IN>
+__device__ __forceinline__ void wave_epilogue(const f32x16 (&acc)[IN][IM], unsigned char* piece, int64_t m, int64_t n,
+                                              int lane, const Epilogue& e) {
+  const int r = lane & 31, g = lane >> 5;
+  wave_epilogue_by<T, IM, IN>(
+      [&](int im, unsigned char* p) {
+#pragma unroll
+        for (int jn = 0; jn < IN; ++jn)
+#pragma unroll
+          for (int vq = 0; vq < 4; ++vq)
+            put_sums<IN>(p, r, 8 * jn + 2 * vq + g,
+                         f32x4{acc[jn][im][4 * vq], acc[jn][im][4 * vq + 1], acc[jn][im][4 * vq + 2], acc[jn][im][4 * vq + 3]});
+      },
+      piece, m, n, lane, e);
 }
 
 // Host: which row tensors move whole pieces

@@ -599,12 +599,11 @@ int launch_shape(TunedGemmArgs a, const E& e, hipStream_t stream) {
 }
 template <bool A_TR, bool B_TR, typename E>
 int launch_form(const TunedGemmArgs& a, const E& e, int shape, hipStream_t stream) {
-  switch (shape) {
-    case 0: return launch_shape<A_TR, B_TR, Tile256x256>(a, e, stream);
-    case 1: return launch_shape<A_TR, B_TR, Tile256x128>(a, e, stream);
-    case 2: return launch_shape<A_TR, B_TR, Tile128x128>(a, e, stream);
-    default: break;
+  if constexpr (!kLinear<E>) {
+    if (shape == 0) return launch_shape<A_TR, B_TR, Tile256x256>(a, e, stream);
+    if (shape == 1) return launch_shape<A_TR, B_TR, Tile256x128>(a, e, stream);
   }
+  if (shape == 2) return launch_shape<A_TR, B_TR, Tile128x128>(a, e, stream);
   if constexpr (A_TR) return -1;
   else return launch_shape<A_TR, B_TR, Tile64x128>(a, e, stream);
 }
@@ -708,10 +707,14 @@ int launch_linear_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const v
   a.slices_per_split = plan.slices_per_split;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (!a_tr && skinny_takes(M, N, K)) return launch_few_rows(b_tr, a, e, st);
-  if (a.splits == 1) return launch_tiles(a_tr, b_tr, a, e, plan.shape, st);
-  a.P = static_cast<float*>(ws);
-  const int rc = launch_tiles(a_tr, b_tr, a, NoEpilogue{}, plan.shape, st);
-  return rc ? rc : launch_linear_epilogue(1, {a.P, N, a.splits}, e, stream);
+  if (a.splits > 1) a.P = static_cast<float*>(ws);
+  int rc;
+  if (plan.shape < 2)
+    rc = launch_linear_tiles(a_tr, b_tr, plan.shape == 0, A, lda, B, ldb, M, N, K, plan.splits, plan.slices_per_split, e, ws, stream);
+  else
+    rc = a.splits == 1 ? launch_tiles(a_tr, b_tr, a, e, plan.shape, st) : launch_tiles(a_tr, b_tr, a, NoEpilogue{}, plan.shape, st);
+  if (rc || a.splits == 1) return rc;
+  return launch_linear_epilogue(1, {a.P, N, a.splits}, e, stream);
 }
 
 }  // namespace mhffn

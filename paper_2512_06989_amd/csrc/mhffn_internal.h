@@ -147,6 +147,10 @@ struct LinearSums {   // Epilogue over `splits` partial products P [splits][M][l
 size_t linear_bf16_workspace_bytes(bool a_tr, int64_t M, int64_t N, int64_t K);
 int launch_linear_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb,
                        int64_t M, int64_t N, int64_t K, const Epilogue& e, void* ws, void* stream);
+// Its large tiles, 256 x 256 (wide) or 256 x 128: the epilogue, or with splits > 1 the partial sums in P
+int launch_linear_tiles(bool a_tr, bool b_tr, bool wide, const void* A, int64_t lda, const void* B, int64_t ldb,
+                        int64_t M, int64_t N, int64_t K, int splits, int64_t slices_per_split,
+                        const Epilogue& e, void* P, void* stream);
 // The same in fp32: any sizes, any strides
 size_t linear_f32_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int launch_linear_f32(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M,
