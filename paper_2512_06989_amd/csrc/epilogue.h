@@ -15,6 +15,8 @@
 #include "mhffn_device.h"
 #include "mhffn_internal.h"
 
+#include <type_traits>
+
 namespace mhffn {
 
 // ---- dropout ----------------------------------------------------------------------------------
@@ -177,6 +179,39 @@ __device__ __forceinline__ void store8(float* p, int cols, bool vec, const float
   }
 }
 
+// A piece as it lies in memory
+template <typename T> struct Raw8 { u32x4 w[sizeof(T) / 2]; };
+__device__ __forceinline__ void unpack8(const Raw8<uint16_t>& r, float (&v)[8]) { unpack8(r.w[0], v); }
+__device__ __forceinline__ void unpack8(const Raw8<float>& r, float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t bits = r.w[j >> 2][j & 3];
+    v[j] = __builtin_bit_cast(float, bits);
+  }
+}
+__device__ __forceinline__ Raw8<uint16_t> load_raw8(const uint16_t* p, int cols, bool vec) {
+  Raw8<uint16_t> r;
+  if (vec && cols >= 8) {
+    r.w[0] = *reinterpret_cast<const u32x4*>(p);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      r.w[0][j] = (2 * j < cols ? (uint32_t)p[2 * j] : 0u) | (2 * j + 1 < cols ? (uint32_t)p[2 * j + 1] << 16 : 0u);
+  }
+  return r;
+}
+__device__ __forceinline__ Raw8<float> load_raw8(const float* p, int cols, bool vec) {
+  Raw8<float> r;
+  if (vec && cols >= 8) {
+    r.w[0] = reinterpret_cast<const u32x4*>(p)[0];
+    r.w[1] = reinterpret_cast<const u32x4*>(p)[1];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r.w[j >> 2][j & 3] = j < cols ? __builtin_bit_cast(uint32_t, p[j]) : 0u;
+  }
+  return r;
+}
+
 // ---- the epilogue of pieces in one column of pieces -------------------------------------------------
 // Columns col .. col + 7 of any row, whose bias is read once.  residual() before finish(), by the
 // same thread: Y may be the residual itself.  Rows and columns that do not exist are left alone.
@@ -191,13 +226,15 @@ struct EpilogueColumns {
     for (int j = 0; j < 8; ++j) bias[j] = 0.f;
     if (e.bias && cols > 0) load8(static_cast<const T*>(e.bias) + col, cols, true, bias);
   }
-  __device__ __forceinline__ void residual(int64_t row, const Epilogue& e, float (&r)[8]) const {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) r[j] = 0.f;
-    if (e.residual && row < e.M && cols > 0) load8(static_cast<const T*>(e.residual) + row * e.ldr + col, cols, e.vec & 2, r);
+  __device__ __forceinline__ Raw8<T> residual(int64_t row, const Epilogue& e) const {
+    if (e.residual && row < e.M && cols > 0) return load_raw8(static_cast<const T*>(e.residual) + row * e.ldr + col, cols, e.vec & 2);
+    return Raw8<T>{};
   }
-  // v: the product's eight sums in, what was stored in Y out
-  __device__ __forceinline__ void finish(float (&v)[8], int64_t row, const float (&r)[8], const Epilogue& e, const DropKey& key) const {
+  __device__ __forceinline__ void store(const float (&v)[8], int64_t row, const Epilogue& e) const {
+    if (row < e.M && cols > 0) store8(static_cast<T*>(e.Y) + row * e.ldy + col, cols, e.vec & 4, v);
+  }
+  // v: the product's eight sums
+  __device__ __forceinline__ void finish(float (&v)[8], int64_t row, const Raw8<T>& res, const Epilogue& e, const DropKey& key) const {
     if (row >= e.M || cols <= 0) return;
     if (e.bias) {
 #pragma unroll
@@ -207,6 +244,8 @@ struct EpilogueColumns {
     activate8<T>(v, e.act);
     drop8(v, (uint64_t)row * (uint64_t)((e.N + 7) >> 3) + (uint64_t)(col >> 3), e.drop, key);
     if (e.residual) {
+      float r[8];
+      unpack8(res, r);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += r[j];
     }
@@ -216,15 +255,14 @@ struct EpilogueColumns {
 template <typename T>
 __device__ __forceinline__ void epilogue8(float (&v)[8], int64_t row, int64_t col, const Epilogue& e, const DropKey& key) {
   const EpilogueColumns<T> ec(e, col);
-  float r[8];
-  ec.residual(row, e, r);
+  const Raw8<T> r = ec.residual(row, e);
   ec.finish(v, row, r, e, key);
 }
 
 // A wave's piece of a product, 32 IM rows m by 32 IN columns n.  The sums pass through LDS in fp32, 32 rows at a time
 // (`piece`, the wave's own 32 x 32 IN floats), so that a lane holds eight columns of one row: whole rows of
 // the residual, Z and Y move, and a call of the generator serves the lane that makes it.
-// `put`(im, piece) stores rows 32 im .. + 31 with put_sums: four columns 4 c .. + 3 of a row, the 16-byte
+// `put`(im, piece), im a compile-time constant, stores rows 32 im .. + 31 with put_sums: four columns 4 c .. + 3 of a row, the 16-byte
 // chunks of a row permuted by the row (no bank meets two lanes on either side).
 template <int IN>
 __device__ __forceinline__ int sums_off(int row, int c) { return row * (128 * IN) + ((c ^ (row & (8 * IN - 1))) << 4); }
@@ -232,27 +270,57 @@ template <int IN>
 __device__ __forceinline__ void put_sums(unsigned char* piece, int row, int c, f32x4 v) {
   *reinterpret_cast<f32x4*>(piece + sums_off<IN>(row, c)) = v;
 }
-template <typename T, int IM, int IN, typename Put>
+// The residual is asked for one group of rows ahead.  The loops stay loops (only `put` needs its row block
+// at compile time): unrolled, an epilogue of 128 x 128 is 150 KB of code.
+template <int I, int N, typename F>
+__device__ __forceinline__ void at_index(int i, F&& f) {
+  if constexpr (I < N) {
+    if (i == I) {   // (the marks keep the compiler from making one block of all, which would index registers)
+      asm volatile("; %0" ::"n"(I));
+      f(std::integral_constant<int, I>{});
+      asm volatile("; %0" ::"n"(I));
+    } else {
+      at_index<I + 1, N>(i, f);
+    }
+  }
+}
+// SUMS: store what is there and nothing else (partial sums).
+template <typename T, int IM, int IN, bool SUMS = false, typename Put>
 __device__ __forceinline__ void wave_epilogue_by(Put&& put, unsigned char* piece, int64_t m, int64_t n, int lane, const Epilogue& e) {
-  constexpr int LPR = 4 * IN, RPP = 64 / LPR, PASSES = 32 / RPP;   // lanes per row, rows per pass
-  const DropKey key = drop_key(e.drop);
+  constexpr int LPR = 4 * IN, RPP = 64 / LPR, PASSES = 32 / RPP, GS = PASSES < 4 ? PASSES : 4;   // lanes per row, rows per pass
+  const DropKey key = SUMS ? DropKey{} : drop_key(e.drop);
   const int lrow = lane / LPR, c = 2 * (lane % LPR);
   const EpilogueColumns<T> ec(e, n + 8 * (lane % LPR));
+  int64_t row = m + lrow;
+  Raw8<T> res[GS];
 #pragma unroll
+  for (int q = 0; q < GS; ++q) res[q] = SUMS ? Raw8<T>{} : ec.residual(row + q * RPP, e);
+#pragma unroll 1
   for (int im = 0; im < IM; ++im) {
-    const int64_t mb = m + 32 * im;
-    float res[PASSES][8];
-#pragma unroll
-    for (int q = 0; q < PASSES; ++q) ec.residual(mb + q * RPP + lrow, e, res[q]);
-    put(im, piece);
+    at_index<0, IM>(im, [&](auto I_) __attribute__((always_inline)) { put(I_, piece); });
     __builtin_amdgcn_wave_barrier();   // (one wave: its reads follow its writes in the same queue)
+#pragma unroll 1
+    for (int p = 0; p < PASSES; p += GS) {
+      Raw8<T> next[GS];
+      const bool more = !SUMS && (im + 1 < IM || p + GS < PASSES);
+      if (more) {
 #pragma unroll
-    for (int q = 0; q < PASSES; ++q) {
-      const int row = q * RPP + lrow;
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(piece + sums_off<IN>(row, c));
-      const f32x4 hi = *reinterpret_cast<const f32x4*>(piece + sums_off<IN>(row, c + 1));
-      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      ec.finish(v, mb + row, res[q], e, key);
+        for (int q = 0; q < GS; ++q) next[q] = ec.residual(row + (GS + q) * RPP, e);
+      }
+#pragma unroll
+      for (int q = 0; q < GS; ++q) {
+        const int r = (p + q) * RPP + lrow;
+        const f32x4 lo = *reinterpret_cast<const f32x4*>(piece + sums_off<IN>(r, c));
+        const f32x4 hi = *reinterpret_cast<const f32x4*>(piece + sums_off<IN>(r, c + 1));
+        float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        if constexpr (SUMS) ec.store(v, row + q * RPP, e);
+        else ec.finish(v, row + q * RPP, res[q], e, key);
+      }
+      row += GS * RPP;
+      if (more) {
+#pragma unroll
+        for (int q = 0; q < GS; ++q) res[q] = next[q];
+      }
     }
     __builtin_amdgcn_wave_barrier();
   }
@@ -264,7 +332,8 @@ __device__ __forceinline__ void wave_epilogue(const f32x16 (&acc)[IN][IM], unsig
                                               int lane, const Epilogue& e) {
   const int r = lane & 31, g = lane >> 5;
   wave_epilogue_by<T, IM, IN>(
-      [&](int im, unsigned char* p) {
+      [&](auto IM_, unsigned char* p) __attribute__((always_inline)) {
+        constexpr int im = decltype(IM_)::value;
 #pragma unroll
         for (int jn = 0; jn < IN; ++jn)
 #pragma unroll

@@ -439,10 +439,9 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_skinny_kernel(Tun
     if (tid >= 128) return;
     const int row = tid >> 2, vq = tid & 3;
     const f32x4 lo4 = red[vq * 64 + row], hi4 = red[vq * 64 + 32 + row];
-    float v[8] = {lo4[0], lo4[1], lo4[2], lo4[3], hi4[0], hi4[1], hi4[2], hi4[3]}, res[8];
+    float v[8] = {lo4[0], lo4[1], lo4[2], lo4[3], hi4[0], hi4[1], hi4[2], hi4[3]};
     EpilogueColumns<uint16_t> ec(e, n0 + 8 * vq);
-    ec.residual(m0 + row, e, res);
-    ec.finish(v, m0 + row, res, e, drop_key(e.drop));
+    ec.finish(v, m0 + row, ec.residual(m0 + row, e), e, drop_key(e.drop));
     return;
   }
   const int64_t m = m0 + (tid & 31), n = n0 + 8 * (tid >> 6) + 4 * ((tid >> 5) & 1);
@@ -540,10 +539,9 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_few_kernel(TunedG
     if (lane >= 32) return;
     const int row = lane >> 1, q = lane & 1;
     const f32x4 lo4 = red[32 * q + row], hi4 = red[32 * q + 16 + row];
-    float v[8] = {lo4[0], lo4[1], lo4[2], lo4[3], hi4[0], hi4[1], hi4[2], hi4[3]}, res[8];
+    float v[8] = {lo4[0], lo4[1], lo4[2], lo4[3], hi4[0], hi4[1], hi4[2], hi4[3]};
     EpilogueColumns<uint16_t> ec(e, n0 + 8 * q);
-    ec.residual(row, e, res);
-    ec.finish(v, row, res, e, drop_key(e.drop));
+    ec.finish(v, row, ec.residual(row, e), e, drop_key(e.drop));
     return;
   }
   if (i16 < a.M)

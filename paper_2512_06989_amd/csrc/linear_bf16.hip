@@ -73,6 +73,11 @@ __device__ __forceinline__ const unsigned char* uniform(const unsigned char* p) 
   return (const unsigned char*)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) |
                                 (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
 }
+// global_to_lds_16B to an LDS address (the same in every lane)
+__device__ __forceinline__ void load_to_lds(const void* gptr, unsigned to) {
+  __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) const void*)gptr,
+                                   (__attribute__((address_space(3))) void*)(uintptr_t)to, 16, 0, 0);
+}
 // byte offset of 16-byte chunk `chunk` of `row` in a row-form unit
 __device__ __forceinline__ int row_unit_off(int row, int chunk) { return row * 128 + ((chunk ^ ((row >> 1) & 7)) << 4); }
 // the chunk bits that k row `kr` of a transposed unit flips
@@ -141,13 +146,12 @@ __global__ __launch_bounds__(512, 2) void linear_gemm_kernel(LinearGemmArgs a, E
       late ? a.A + (A_TR ? m0 + kbase * kSlice * a.lda : m0 * a.lda + kbase * kSlice)
            : a.B + (B_TR ? n0 + kbase * kSlice * a.ldb : n0 * a.ldb + kbase * kSlice)));
   const int64_t gstep = late ? (A_TR ? a.lda : 1) * (RA::kK * 2) : (B_TR ? a.ldb : 1) * (RB::kK * 2);
-  unsigned char* const ring_a = smem;
-  unsigned char* const ring_b = smem + RA::kBytes;
-  auto request_side = [&](auto TR_, auto ring_, unsigned char* ring, int unit, int slot) {
+  const unsigned ring_a = lds_addr_of(smem), ring_b = ring_a + RA::kBytes;   // LDS addresses
+  auto request_side = [&](auto TR_, auto ring_, unsigned ring, int unit, int slot) {
     using R = typename decltype(ring_)::type;
     constexpr bool TR = decltype(TR_)::value;
     const unsigned char* const p = gbase + unit * gstep;
-    unsigned char* const to = ring + slot * R::kUnit + w4 * 1024;
+    const unsigned to = ring + slot * R::kUnit + w4 * 1024;
     const bool cut = TR ? A_TR && k_left < kSlice && kbase + unit == KT_all - 1 : kbase + 2 * unit + 1 >= KT_all;
     if (__builtin_expect(cut, 0)) {   // (this side's last request: its offsets are overwritten)
 #pragma unroll
@@ -157,7 +161,7 @@ __global__ __launch_bounds__(512, 2) void linear_gemm_kernel(LinearGemmArgs a, E
       }
     }
 #pragma unroll
-    for (int q = 0; q < R::kLoads; ++q) global_to_lds_16B(p + goff[q], to + q * 4096);
+    for (int q = 0; q < R::kLoads; ++q) load_to_lds(p + goff[q], to + q * 4096);
   };
   struct SideA { using type = RA; };
   struct SideB { using type = RB; };
@@ -184,7 +188,7 @@ __global__ __launch_bounds__(512, 2) void linear_gemm_kernel(LinearGemmArgs a, E
   unsigned at[2][kRegs];   // [m side]
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
-    const unsigned base = lds_addr_of(side ? ring_a : ring_b), wrow = side ? G::TM * wm : G::TN * wn;
+    const unsigned base = side ? ring_a : ring_b, wrow = side ? G::TM * wm : G::TN * wn;
     const int kr = 8 * gq + (i16 >> 2);
 #pragma unroll
     for (int x = 0; x < kRegs; ++x)
@@ -290,8 +294,9 @@ __global__ __launch_bounds__(512, 2) void linear_gemm_kernel(LinearGemmArgs a, E
   if (!late) barrier();
   __syncthreads();   // the rings are done with
   if (sizeof(T) == 4) e.Y = static_cast<float*>(e.Y) + (int64_t)split * a.M * a.N;
-  wave_epilogue_by<T, IM / 2, IN / 2>(
-      [&](int im, unsigned char* piece) {
+  wave_epilogue_by<T, IM / 2, IN / 2, sizeof(T) == 4>(
+      [&](auto IM_, unsigned char* piece) __attribute__((always_inline)) {
+        constexpr int im = decltype(IM_)::value;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
