@@ -391,6 +391,20 @@ size_t mhffn_linear_workspace_bytes(const mhffn_linear_desc* desc, int op) {
   return mhffn::linear_workspace_bytes(p, op == MHFFN_OP_LINEAR_BACKWARD);
 }
 
+// Not part of the interface, like mhffn_plan_text: what a call with 16-byte aligned operands would launch
+int mhffn_linear_plan_text(const mhffn_linear_desc* desc, int op, char* text, size_t size) {
+  if (!text || size == 0) return MHFFN_ERR_NULL;
+  text[0] = 0;
+  mhffn::Linear p;
+  const int rc = check_linear(desc, nullptr, &p);
+  if (rc || p.M == 0) return rc;
+  if (op != MHFFN_OP_LINEAR_FORWARD && op != MHFFN_OP_LINEAR_BACKWARD) return MHFFN_ERR_UNSUPPORTED;
+  const std::string plan = mhffn::linear_plan(p, op == MHFFN_OP_LINEAR_BACKWARD);
+  strncpy(text, plan.c_str(), size - 1);
+  text[size - 1] = 0;
+  return MHFFN_OK;
+}
+
 int mhffn_linear_forward(const mhffn_linear_desc* desc, const void* X, const void* W, const void* bias,
                          const void* residual, const void* rng, void* Y, void* Z, void* workspace,
                          size_t workspace_bytes, void* hip_stream) {

@@ -50,7 +50,7 @@ struct TunedGemmArgs {
   // slices of k each; they leave fp32 partial tiles in P [splits][M][N]
   int splits;
   int64_t slices_per_split;
-  float* P;         // NULL: one workgroup per tile, which stores C
+  float* P;
   int accumulate;   // add to what C holds (one more rounding to bf16)
 };
 
@@ -81,12 +81,8 @@ using Tile64x128 = GemmTile<64, 128, 2, 2, 5>;   // (m side in row form: a trans
 // byte offset of 16-byte chunk `chunk` of `row` in a row-form image
 __device__ __forceinline__ int row_image_off(int row, int chunk) { return row * 64 + ((chunk ^ ((row >> 2) & 3)) << 4); }
 
-// What a product's kernel does with its sums: stores them in C (or adds to it), or the linear layer's epilogue
-struct NoEpilogue {};
-template <typename E> constexpr bool kLinear = std::is_same<E, Epilogue>::value;
-
-template <bool A_TR, bool B_TR, typename G, typename E>
-__global__ __launch_bounds__(64 * G::NW, G::BM == 256 ? 2 : 4) void gemm_bf16_kernel(TunedGemmArgs a, E e) {
+template <bool A_TR, bool B_TR, typename G>
+__global__ __launch_bounds__(64 * G::NW, G::BM == 256 ? 2 : 4) void gemm_bf16_kernel(TunedGemmArgs a) {
   constexpr int IM = G::IM, IN = G::IN, S = G::S, NW = G::NW;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -256,12 +252,7 @@ __global__ __launch_bounds__(64 * G::NW, G::BM == 256 ? 2 : 4) void gemm_bf16_ke
   });
 
   // ---- store: lane = row m, registers = four consecutive n per group ----------------------
-  if constexpr (kLinear<E>) {
-    __syncthreads();                                   // the stages are done with
-    wave_epilogue<uint16_t, IM, IN>(acc, smem + wave * (32 * G::TN * 4), m0 + G::TM * wm, n0 + G::TN * wn, lane, e);
-    return;
-  }
-  if (a.P || a.accumulate) {
+  if (a.splits > 1 || a.accumulate) {
 #pragma unroll
     for (int im = 0; im < IM; ++im) {
       const int64_t m = m0 + G::TM * wm + 32 * im + r;
@@ -274,7 +265,7 @@ __global__ __launch_bounds__(64 * G::NW, G::BM == 256 ? 2 : 4) void gemm_bf16_ke
           if (n + 4 > a.N) continue;
           float o[4] = {acc[jn][im][4 * vq], acc[jn][im][4 * vq + 1], acc[jn][im][4 * vq + 2],
                         acc[jn][im][4 * vq + 3]};
-          if (a.P) {
+          if (a.splits > 1) {
             *reinterpret_cast<f32x4*>(a.P + ((size_t)split * a.M + m) * a.N + n) = f32x4{o[0], o[1], o[2], o[3]};
             continue;
           }
@@ -341,6 +332,10 @@ __global__ void gemm_bf16_reduce_kernel(TunedGemmArgs a) {
   pk[1] = pack_bf16(sum[2], sum[3]);
   *dst = pk;
 }
+
+// What the kernels for few rows do with their sums: store them in C, or the linear layer's epilogue
+struct NoEpilogue {};
+template <typename E> constexpr bool kLinear = std::is_same<E, Epilogue>::value;
 
 // ---------------------------------------------------------------------------
 // Few rows (decoding): C[M][N] = A[M][K] B, A row form, B in either form.  The weights are read
@@ -581,37 +576,32 @@ GemmPlan plan_tiles(bool a_tr, int64_t M, int64_t N, int64_t K) {
   return best;
 }
 
-template <bool A_TR, bool B_TR, typename G, typename E>
-int launch_shape(TunedGemmArgs a, const E& e, hipStream_t stream) {
+template <bool A_TR, bool B_TR, typename G>
+int launch_shape(TunedGemmArgs a, hipStream_t stream) {
   a.tiles_n = (a.N + G::BN - 1) / G::BN;
   a.n_items = ((a.M + G::BM - 1) / G::BM) * a.tiles_n * a.splits;
-  if (hipError_t e0 = LdsLimit<&gemm_bf16_kernel<A_TR, B_TR, G, E>, G::kLds>::ensure(); e0 != hipSuccess) return (int)e0;
-  hipLaunchKernelGGL((gemm_bf16_kernel<A_TR, B_TR, G, E>), dim3((unsigned)xcd_grid_size(a.n_items)), dim3(64 * G::NW),
-                     G::kLds, stream, a, e);
-  const hipError_t rc = hipGetLastError();
-  if (rc != hipSuccess || a.splits == 1 || !a.C) return (int)rc;
+  if (hipError_t e0 = LdsLimit<&gemm_bf16_kernel<A_TR, B_TR, G>, G::kLds>::ensure(); e0 != hipSuccess) return (int)e0;
+  hipLaunchKernelGGL((gemm_bf16_kernel<A_TR, B_TR, G>), dim3((unsigned)xcd_grid_size(a.n_items)), dim3(64 * G::NW),
+                     G::kLds, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.splits == 1) return (int)e;
   const int64_t n4 = a.M * a.N / 4;
   hipLaunchKernelGGL(gemm_bf16_reduce_kernel, dim3((unsigned)((n4 + 255) / 256)), dim3(256), 0,
                      stream, a);
   return (int)hipGetLastError();
 }
-template <bool A_TR, bool B_TR, typename E>
-int launch_form(const TunedGemmArgs& a, const E& e, int shape, hipStream_t stream) {
-  if constexpr (!kLinear<E>) {
-    if (shape == 0) return launch_shape<A_TR, B_TR, Tile256x256>(a, e, stream);
-    if (shape == 1) return launch_shape<A_TR, B_TR, Tile256x128>(a, e, stream);
+template <bool A_TR, bool B_TR>
+int launch_form(const TunedGemmArgs& a, int shape, hipStream_t stream) {
+  switch (shape) {
+    case 0: return launch_shape<A_TR, B_TR, Tile256x256>(a, stream);
+    case 1: return launch_shape<A_TR, B_TR, Tile256x128>(a, stream);
+    case 2: return launch_shape<A_TR, B_TR, Tile128x128>(a, stream);
+    default: break;
   }
-  if (shape == 2) return launch_shape<A_TR, B_TR, Tile128x128>(a, e, stream);
   if constexpr (A_TR) return -1;
-  else return launch_shape<A_TR, B_TR, Tile64x128>(a, e, stream);
+  else return launch_shape<A_TR, B_TR, Tile64x128>(a, stream);
 }
-template <typename E>
-int launch_tiles(bool a_tr, bool b_tr, const TunedGemmArgs& a, const E& e, int shape, hipStream_t stream) {
-  if (!a_tr && b_tr) return launch_form<false, true>(a, e, shape, stream);
-  if (!a_tr && !b_tr) return launch_form<false, false>(a, e, shape, stream);
-  if (a_tr && b_tr) return launch_form<true, true>(a, e, shape, stream);
-  return -1;   // transposed A with row-form B: no caller
-}
+
 template <typename E>
 int launch_few_rows(bool b_tr, const TunedGemmArgs& a, const E& e, hipStream_t stream) {
   if (few_takes(b_tr, a.M)) return b_tr ? launch_few<true>(a, e, stream) : launch_few<false>(a, e, stream);
@@ -680,39 +670,23 @@ int launch_gemm_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const voi
   a.tiles_n = 0; a.n_items = 0;
   a.splits = plan.splits;
   a.slices_per_split = plan.slices_per_split;
-  a.P = plan.splits > 1 ? static_cast<float*>(ws) : nullptr;
+  a.P = static_cast<float*>(ws);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (!a_tr && skinny_takes(M, N, K) && !accumulate) return launch_few_rows(b_tr, a, NoEpilogue{}, st);
   if (a.splits > 1 && !ws) return -1;
-  return launch_tiles(a_tr, b_tr, a, NoEpilogue{}, plan.shape, st);
+  if (!a_tr && b_tr) return launch_form<false, true>(a, plan.shape, st);
+  if (!a_tr && !b_tr) return launch_form<false, false>(a, plan.shape, st);
+  if (a_tr && b_tr) return launch_form<true, true>(a, plan.shape, st);
+  return -1;   // transposed A with row-form B: no caller
 }
 
-size_t linear_bf16_workspace_bytes(bool a_tr, int64_t M, int64_t N, int64_t K) {
-  if (!a_tr && skinny_takes(M, N, K)) return 0;
-  const int splits = plan_tiles(a_tr, M, N, K).splits;
-  return splits > 1 ? (size_t)splits * M * N * sizeof(float) : 0;
-}
-
-int launch_linear_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M,
-                       int64_t N, int64_t K, const Epilogue& e0, void* ws, void* stream) {
-  const Epilogue e = with_vec(e0, 1);
-  const GemmPlan plan = plan_tiles(a_tr, M, N, K);
+int launch_linear_few_rows(bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N, int64_t K,
+                           const Epilogue& e, void* stream) {
   TunedGemmArgs a = {};
   a.A = static_cast<const uint16_t*>(A);
   a.B = static_cast<const uint16_t*>(B);
   a.M = M; a.N = N; a.K = K; a.lda = lda; a.ldb = ldb;
-  a.splits = plan.splits;
-  a.slices_per_split = plan.slices_per_split;
-  hipStream_t st = static_cast<hipStream_t>(stream);
-  if (!a_tr && skinny_takes(M, N, K)) return launch_few_rows(b_tr, a, e, st);
-  if (a.splits > 1) a.P = static_cast<float*>(ws);
-  int rc;
-  if (plan.shape < 2)
-    rc = launch_linear_tiles(a_tr, b_tr, plan.shape == 0, A, lda, B, ldb, M, N, K, plan.splits, plan.slices_per_split, e, ws, stream);
-  else
-    rc = a.splits == 1 ? launch_tiles(a_tr, b_tr, a, e, plan.shape, st) : launch_tiles(a_tr, b_tr, a, NoEpilogue{}, plan.shape, st);
-  if (rc || a.splits == 1) return rc;
-  return launch_linear_epilogue(1, {a.P, N, a.splits}, e, stream);
+  return launch_few_rows(b_tr, a, with_vec(e, 1), static_cast<hipStream_t>(stream));
 }
 
 }  // namespace mhffn

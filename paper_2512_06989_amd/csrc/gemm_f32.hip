@@ -184,6 +184,11 @@ int launch_form(bool a_tr, bool b_tr, const GemmF32Args& a, const Epilogue& e, h
 
 }  // namespace
 
+std::string linear_f32_plan(int64_t M, int64_t N, int64_t K) {
+  const F32Plan p = plan_f32(M, N, K);
+  return std::to_string(p.tile) + "x" + std::to_string(p.tile) + " splits=" + std::to_string(p.splits);
+}
+
 size_t linear_f32_workspace_bytes(int64_t M, int64_t N, int64_t K) {
   const int splits = plan_f32(M, N, K).splits;
   return splits > 1 ? (size_t)splits * M * N * sizeof(float) : 0;

@@ -39,8 +39,8 @@ struct Operands {
   int64_t ldz(const Linear& p) const { return p.dtype == 1 ? Np : p.N; }
 };
 
-size_t partial_bytes(int dtype, bool a_tr, int64_t M, int64_t N, int64_t K) {
-  return dtype == 1 ? linear_bf16_workspace_bytes(a_tr, M, N, K) : linear_f32_workspace_bytes(M, N, K);
+size_t partial_bytes(int dtype, bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K) {
+  return dtype == 1 ? linear_bf16_workspace_bytes(a_tr, b_tr, M, N, K) : linear_f32_workspace_bytes(M, N, K);
 }
 
 // Epilogue e over A B
@@ -48,6 +48,9 @@ int product(int dtype, bool a_tr, bool b_tr, const void* A, int64_t lda, const v
             int64_t N, int64_t K, float* P, const Epilogue& e, void* stream) {
   return (dtype == 1 ? launch_linear_bf16 : launch_linear_f32)(a_tr, b_tr, A, lda, B, ldb, M, N, K, e, P, stream);
 }
+
+// Columns that the forward's product works on: with W packed its padding is there for the asking
+int64_t forward_columns(const Linear& p, const Operands& o) { return p.dtype != 1 ? p.N : o.w ? o.Np : up(p.N, 8); }
 
 Epilogue plain(void* Y, int64_t ldy, int64_t M, int64_t N) {
   Epilogue e = {};
@@ -62,8 +65,8 @@ int forward(const Linear& p, const void* X, const void* W, const void* bias, con
   Arena arena{static_cast<unsigned char*>(ws)};
   void* const Xp = o.x ? arena.take((size_t)p.M * o.Kp * 2) : nullptr;
   void* const Wp = o.w ? arena.take((size_t)o.Kp * o.Np * 2) : nullptr;
-  const int64_t K = o.x || o.w ? o.Kp : p.K, N = bf16 ? up(p.N, 8) : p.N;
-  float* const P = static_cast<float*>(arena.take(partial_bytes(p.dtype, false, p.M, N, K)));
+  const int64_t K = bf16 && (o.x || o.w) ? o.Kp : p.K, N = forward_columns(p, o);
+  float* const P = static_cast<float*>(arena.take(partial_bytes(p.dtype, false, true, p.M, N, K)));
   if (bytes) {
     *bytes = arena.used;
     return 0;
@@ -93,7 +96,7 @@ int backward(const Linear& p, const void* X, const void* W, const void* Z, const
   const int64_t Nk = bf16 ? o.Np : p.N;   // the contraction of dX
   void* const dZ = o.dz ? arena.take((size_t)p.M * ldz * elt(p.dtype)) : nullptr;
   float* const sums = static_cast<float*>(arena.take((size_t)linear_column_blocks(p.M, p.N) * p.N * 4));
-  const size_t px = partial_bytes(p.dtype, false, p.M, K8, Nk), pw = partial_bytes(p.dtype, true, K8, N8, p.M);
+  const size_t px = partial_bytes(p.dtype, false, false, p.M, K8, Nk), pw = partial_bytes(p.dtype, true, true, K8, N8, p.M);
   float* const P = static_cast<float*>(arena.take(px > pw ? px : pw));
   if (bytes) {
     *bytes = arena.used;
@@ -119,6 +122,20 @@ int backward(const Linear& p, const void* X, const void* W, const void* Z, const
 }
 
 }  // namespace
+
+std::string linear_plan(const Linear& p, bool back) {
+  const Operands o(p, back);
+  std::string s = o.x ? "packed X " : "";
+  if (o.w) s += "packed W ";
+  if (o.dz) s += "dZ ";
+  auto plan = [&](bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K) {
+    return p.dtype == 1 ? linear_bf16_plan(a_tr, b_tr, M, N, K) : linear_f32_plan(M, N, K);
+  };
+  const bool bf16 = p.dtype == 1;
+  const int64_t K8 = bf16 ? up(p.K, 8) : p.K, N8 = bf16 ? up(p.N, 8) : p.N;
+  if (!back) return s + plan(false, true, p.M, forward_columns(p, o), o.x || o.w ? o.Kp : p.K);
+  return s + "dX " + plan(false, false, p.M, K8, bf16 ? o.Np : p.N) + "; dW " + plan(true, true, K8, N8, p.M);
+}
 
 size_t linear_workspace_bytes(const Linear& p, bool back) {
   size_t bytes = 0;

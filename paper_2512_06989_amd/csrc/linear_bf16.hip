@@ -27,7 +27,7 @@
 namespace mhffn {
 namespace {
 
-constexpr int kSlice = 32;      // k per half step
+constexpr int kStep = 32;      // k per half step
 constexpr uint32_t kBand = 4;   // tiles along n that are worked on side by side
 
 struct LinearGemmArgs {
@@ -83,6 +83,25 @@ __device__ __forceinline__ int row_unit_off(int row, int chunk) { return row * 1
 // the chunk bits that k row `kr` of a transposed unit flips
 __device__ __forceinline__ int tr_flip(int kr) { return (kr & 2) | ((kr >> 1) & 4); }
 
+// A workgroup's tile and share of k.  An XCD's share of the list runs over the tiles of one share of k, in bands
+// of kBand tiles along n: the 32 workgroups that run at once there form a patch of about 4 x 8 tiles, whose 12
+// panels meet in its L2.
+template <typename G>
+__device__ __forceinline__ bool place_of(const LinearGemmArgs& a, int64_t& m0, int64_t& n0, int& split, int64_t& kbase, int64_t& kend) {
+  const int64_t item = xcd_work_item(blockIdx.x, a.n_items);
+  if (item >= a.n_items) return false;
+  const uint32_t n_tiles = (uint32_t)(a.n_items / a.splits), t = (uint32_t)(item % n_tiles);
+  split = (int)(item / n_tiles);
+  const uint32_t tiles_n = (uint32_t)a.tiles_n, tiles_m = n_tiles / tiles_n, band = t / (tiles_m * kBand);
+  const uint32_t width = min(kBand, tiles_n - band * kBand), in_band = t - band * (tiles_m * kBand);
+  m0 = (int64_t)(in_band / width) * G::BM;
+  n0 = (int64_t)(band * kBand + in_band % width) * G::BN;
+  const int64_t KT_all = (a.K + kStep - 1) / kStep;
+  kbase = split * a.slices_per_split;
+  kend = kbase + a.slices_per_split < KT_all ? kbase + a.slices_per_split : KT_all;
+  return true;
+}
+
 // T: what the epilogue stores (fp32: partial sums)
 template <bool A_TR, bool B_TR, typename G, typename T>
 __global__ __launch_bounds__(512, 2) void linear_gemm_kernel(LinearGemmArgs a, Epilogue e) {
@@ -94,18 +113,10 @@ __global__ __launch_bounds__(512, 2) void linear_gemm_kernel(LinearGemmArgs a, E
   const int i16 = lane & 15, gq = lane >> 4;
   const int w4 = wave & 3, wm = wave / G::WN, wn = wave % G::WN;
   const bool late = wave >= 4;
-  const int64_t item = xcd_work_item(blockIdx.x, a.n_items);
-  if (item >= a.n_items) return;
-  // An XCD's share of the list runs over the tiles of one share of k, in bands of kBand tiles along n: the 32
-  // workgroups that run at once there form a patch of about 4 x 8 tiles, whose 12 panels meet in its L2.
-  const uint32_t n_tiles = (uint32_t)(a.n_items / a.splits), t = (uint32_t)(item % n_tiles);
-  const int split = (int)(item / n_tiles);
-  const uint32_t tiles_n = (uint32_t)a.tiles_n, tiles_m = n_tiles / tiles_n, band = t / (tiles_m * kBand);
-  const uint32_t width = min(kBand, tiles_n - band * kBand), in_band = t - band * (tiles_m * kBand);
-  const int64_t m0 = (int64_t)(in_band / width) * G::BM, n0 = (int64_t)(band * kBand + in_band % width) * G::BN;
-  const int64_t K = a.K, KT_all = (K + kSlice - 1) / kSlice;
-  const int64_t kbase = split * a.slices_per_split;           // first slice of this workgroup
-  const int64_t kend = kbase + a.slices_per_split < KT_all ? kbase + a.slices_per_split : KT_all;
+  int64_t m0, n0, kbase, kend;   // tile, slices of k
+  int split;
+  if (!place_of<G>(a, m0, n0, split, kbase, kend)) return;
+  const int64_t K = a.K, KT_all = (K + kStep - 1) / kStep;
   const int KT = (int)(kend - kbase);                         // its number of slices (>= 1)
 
   // ---- requests: a wave has one side, and of its units the 1 KB images 4 q + w4 ----------------
@@ -115,14 +126,14 @@ __global__ __launch_bounds__(512, 2) void linear_gemm_kernel(LinearGemmArgs a, E
   // (their slots are cleared before use).  A request is a wave-uniform base and a 32-bit offset per lane.
   constexpr int kMostLoads = RA::kLoads > RB::kLoads ? RA::kLoads : RB::kLoads;
   const int64_t ld = late ? a.lda : a.ldb, row0 = late ? m0 : n0, rows = late ? a.M : a.N;
-  const int64_t k_left = K - (KT_all - 1) * kSlice;
+  const int64_t k_left = K - (KT_all - 1) * kStep;
   unsigned goff[kMostLoads];
   auto place = [&](auto TR_, int q, int64_t most_k) -> unsigned {   // most_k: k of the unit that exist
     const int img = 4 * q + w4;
     if constexpr (!decltype(TR_)::value) {
       const int row = 8 * img + (lane >> 3);
       int chunk = (lane & 7) ^ ((row >> 1) & 7);
-      if (most_k <= kSlice) chunk &= 3;
+      if (most_k <= kStep) chunk &= 3;
       const int64_t gr = row0 + row < rows ? row : rows - 1 - row0;
       return (unsigned)(gr * ld * 2 + (chunk << 4));
     } else {
@@ -143,8 +154,8 @@ __global__ __launch_bounds__(512, 2) void linear_gemm_kernel(LinearGemmArgs a, E
     for (int q = 0; q < RB::kLoads; ++q) goff[q] = place(TB{}, q, 64);
   }
   const unsigned char* const gbase = uniform(reinterpret_cast<const unsigned char*>(
-      late ? a.A + (A_TR ? m0 + kbase * kSlice * a.lda : m0 * a.lda + kbase * kSlice)
-           : a.B + (B_TR ? n0 + kbase * kSlice * a.ldb : n0 * a.ldb + kbase * kSlice)));
+      late ? a.A + (A_TR ? m0 + kbase * kStep * a.lda : m0 * a.lda + kbase * kStep)
+           : a.B + (B_TR ? n0 + kbase * kStep * a.ldb : n0 * a.ldb + kbase * kStep)));
   const int64_t gstep = late ? (A_TR ? a.lda : 1) * (RA::kK * 2) : (B_TR ? a.ldb : 1) * (RB::kK * 2);
   const unsigned ring_a = lds_addr_of(smem), ring_b = ring_a + RA::kBytes;   // LDS addresses
   auto request_side = [&](auto TR_, auto ring_, unsigned ring, int unit, int slot) {
@@ -152,7 +163,7 @@ __global__ __launch_bounds__(512, 2) void linear_gemm_kernel(LinearGemmArgs a, E
     constexpr bool TR = decltype(TR_)::value;
     const unsigned char* const p = gbase + unit * gstep;
     const unsigned to = ring + slot * R::kUnit + w4 * 1024;
-    const bool cut = TR ? A_TR && k_left < kSlice && kbase + unit == KT_all - 1 : kbase + 2 * unit + 1 >= KT_all;
+    const bool cut = TR ? A_TR && k_left < kStep && kbase + unit == KT_all - 1 : kbase + 2 * unit + 1 >= KT_all;
     if (__builtin_expect(cut, 0)) {   // (this side's last request: its offsets are overwritten)
 #pragma unroll
       for (int q = 0; q < R::kLoads; ++q) {
@@ -253,7 +264,7 @@ __global__ __launch_bounds__(512, 2) void linear_gemm_kernel(LinearGemmArgs a, E
       }
     });
     barrier();
-    const bool ragged_last = A_TR && (kbase + kt == KT_all - 1) && k_left < kSlice;
+    const bool ragged_last = A_TR && (kbase + kt == KT_all - 1) && k_left < kStep;
     if constexpr (A_TR) {
       if (ragged_last) {   // k rows past K were clamped: clear their slots
         static_for<0, OPS>([&](auto C_) {
@@ -305,38 +316,320 @@ __global__ __launch_bounds__(512, 2) void linear_gemm_kernel(LinearGemmArgs a, E
       smem + wave * (32 * G::TN * 4), m0 + G::TM * wm, n0 + G::TN * wn, lane, e);
 }
 
-template <bool A_TR, bool B_TR, int BM, int BN, int WM, int WN, typename T>
+// ---------------------------------------------------------------------------
+// Smaller tiles, for outputs that would leave CUs without one: two rows of waves, k in units of 64.  Such products wait for memory, so what counts is bytes in flight: units lie in a ring that
+// fills LDS (five of 32 KB .. ten of 16 KB), all but one of them under way.  A wave multiplies a unit's operands from
+// registers and between the products reads the next one's from LDS and requests another, an instruction at a
+// time; one wait for LDS and one barrier per unit (two steps of 32 with a wait each: 730 clocks a unit of 64 x 64).
+// Images and operands as above, a transposed unit [64 k][64] per 64 columns.
+// ---------------------------------------------------------------------------
+template <int BM_, int BN_, int WN_, int NK_>
+struct SmallTile {
+  static constexpr int BM = BM_, BN = BN_, WN = WN_, NW = 2 * WN, TM = BM / 2, TN = BN / WN, IM = TM / 16, IN = TN / 16;
+  static constexpr int NK = NK_, kK = 64 * NK;             // k of a unit: NK images [..][64 k] of each side
+  static constexpr int kSubA = BM * 128, kSubB = BN * 128, kUnitA = NK * kSubA, kUnit = NK * (kSubA + kSubB);
+  static constexpr int kSlots = (int)kLdsBytesPerWorkgroup / kUnit, kLds = kSlots * kUnit;
+  static constexpr int kLoadsA = kUnitA / 1024 / NW, kLoadsB = NK * kSubB / 1024 / NW, kLoads = kLoadsA + kLoadsB;   // 1 KB loads per unit of each wave
+  static_assert(BM % 64 == 0 && BN % 64 == 0 && TN % 32 == 0 && kLds >= NW * 32 * TN * 4 && kLoads * (kSlots - 1) < 64, "");
+  static_assert(kLoadsA * NW * 1024 == kUnitA && kLoads * NW * 1024 == kUnit, "whole loads");
+};
+
+template <bool A_TR, bool B_TR, typename G, typename T>
+__global__ __launch_bounds__(64 * G::NW, G::NW / 4) void linear_small_kernel(LinearGemmArgs a, Epilogue e) {
+  constexpr int IM = G::IM, IN = G::IN, OPS = IM + IN, NM = IM * IN, S = G::kSlots, NS = 2 * G::NK;   // operands and products of 32 k, of which a unit has NS
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i16 = lane & 15, gq = lane >> 4;
+  const int wm = wave / G::WN, wn = wave % G::WN;
+  int64_t m0, n0, kbase, kend;
+  int split;
+  if (!place_of<G>(a, m0, n0, split, kbase, kend)) return;
+  const int64_t K = a.K, k0 = kbase * kStep, k_own = (kend * kStep < K ? kend * kStep : K) - k0;
+  const int units = (int)((kend - kbase + NS - 1) / NS);
+
+  // ---- requests: of a side's 1 KB images wave w moves NW q + w -------------------------------------
+  // k past the product's end: row form fetches the unit's first 64, or the first 32 of 64, again, k rows repeat the last.
+  unsigned ga[G::kLoadsA], gb[G::kLoadsB];
+  auto place = [&](bool tr, int q, int64_t ld, int64_t row0, int64_t rows, int images, int64_t left) __attribute__((always_inline)) -> unsigned {
+    const int img = G::NW * q + wave, sub = img / images, i = img % images;   // images: 1 KB images of 64 k of this side
+    int64_t most_k = left - 64 * sub;                                          // k of them that exist
+    if (!tr) {
+      const int row = 8 * i + (lane >> 3), k = most_k > 0 ? 64 * sub : 0;
+      int chunk = (lane & 7) ^ ((row >> 1) & 7);
+      if (most_k <= kStep) chunk &= 3;
+      const int64_t gr = row0 + row < rows ? row : rows - 1 - row0;
+      return (unsigned)((gr * ld + k) * 2 + (chunk << 4));
+    }
+    int64_t kr = 8 * (i & 7) + (lane >> 3);
+    int64_t gc = row0 + 64 * (i >> 3) + (((lane & 7) ^ tr_flip((int)kr)) << 3);
+    gc = (gc + 8 <= rows ? gc : rows - 8) - row0;
+    kr += 64 * sub;
+    kr = kr < left ? kr : left - 1;
+    return (unsigned)((kr * ld + gc) * 2);
+  };
+  auto offsets = [&](int64_t left) __attribute__((always_inline)) {
+#pragma unroll
+    for (int q = 0; q < G::kLoadsA; ++q) ga[q] = place(A_TR, q, a.lda, m0, a.M, G::kSubA / 1024, left);
+#pragma unroll
+    for (int q = 0; q < G::kLoadsB; ++q) gb[q] = place(B_TR, q, a.ldb, n0, a.N, G::kSubB / 1024, left);
+  };
+  const unsigned char* pa = uniform(reinterpret_cast<const unsigned char*>(a.A + (A_TR ? m0 + k0 * a.lda : m0 * a.lda + k0)));
+  const unsigned char* pb = uniform(reinterpret_cast<const unsigned char*>(a.B + (B_TR ? n0 + k0 * a.ldb : n0 * a.ldb + k0)));
+  const int64_t step_a = (A_TR ? a.lda : 1) * (2 * G::kK), step_b = (B_TR ? a.ldb : 1) * (2 * G::kK);
+  const unsigned ring = lds_addr_of(smem);
+  unsigned to = ring + wave * 1024;
+  auto begin = [&](int unit) __attribute__((always_inline)) {
+    const int64_t left = K - k0 - G::kK * (int64_t)unit;
+    if (__builtin_expect(left < G::kK, 0)) {   // (the last request: its offsets take the place of the others')
+      offsets(left);
+#pragma unroll
+      for (int q = 0; q < G::kLoadsA; ++q) asm volatile("" : "+v"(ga[q]));   // (computed here and not ahead of the loop)
+#pragma unroll
+      for (int q = 0; q < G::kLoadsB; ++q) asm volatile("" : "+v"(gb[q]));
+    }
+  };
+  auto load = [&](auto Q_) __attribute__((always_inline)) {
+    constexpr int q = decltype(Q_)::value;
+    if constexpr (q < G::kLoadsA) load_to_lds(pa + ga[q], to + q * (1024 * G::NW));
+    else load_to_lds(pb + gb[q - G::kLoadsA], to + G::kUnitA + (q - G::kLoadsA) * (1024 * G::NW));
+  };
+  auto end = [&]() __attribute__((always_inline)) {
+    pa += step_a;
+    pb += step_b;
+    to = to == ring + (S - 1) * G::kUnit + wave * 1024 ? ring + wave * 1024 : to + G::kUnit;
+  };
+  offsets(G::kK);
+
+  // ---- operands (see above); a transposed unit's halves of k are 4096 bytes apart -----------------------
+  constexpr int RA = A_TR ? IM : 2, RB = B_TR ? IN : 2;
+  unsigned at_a[RA], at_b[RB];
+  auto first = [&](bool tr, unsigned base, unsigned wrow, int x) __attribute__((always_inline)) -> unsigned {
+    const int kr = 8 * gq + (i16 >> 2);
+    return tr ? base + (wrow >> 6) * 8192 + kr * 128 + (((2 * (((wrow & 63) >> 4) + x) + ((i16 >> 1) & 1)) ^ tr_flip(kr)) << 4) + 8 * (i16 & 1)
+              : base + row_unit_off(wrow + i16, gq + 4 * x);
+  };
+#pragma unroll
+  for (int x = 0; x < RA; ++x) at_a[x] = first(A_TR, ring, G::TM * wm, x);
+#pragma unroll
+  for (int x = 0; x < RB; ++x) at_b[x] = first(B_TR, ring + G::kUnitA, G::TN * wn, x);
+  int slot = 0;
+  auto next_unit = [&]() __attribute__((always_inline)) {
+    const unsigned by = slot == S - 1 ? 0u - (S - 1) * G::kUnit : (unsigned)G::kUnit;
+    slot = slot == S - 1 ? 0 : slot + 1;
+#pragma unroll
+    for (int x = 0; x < RA; ++x) at_a[x] += by;
+#pragma unroll
+    for (int x = 0; x < RB; ++x) at_b[x] += by;
+  };
+
+  f32x4 acc[IN][IM];
+#pragma unroll
+  for (int i = 0; i < IN; ++i)
+#pragma unroll
+    for (int j = 0; j < IM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  struct Operands {   // of a unit, 32 k after 32 k
+    s16x4 lo[NS * OPS], hi[NS * OPS];
+    bf16x8 full[NS * OPS];
+  };
+  Operands f0, f1;
+  auto read = [&](auto C_, Operands& f) __attribute__((always_inline)) {
+    constexpr int c = decltype(C_)::value, sub = c / OPS / 2, HALF = c / OPS % 2, o = c % OPS, idx = o < IN ? o : o - IN;
+    constexpr int off = sub * (o < IN ? G::kSubB : G::kSubA);
+    if constexpr (o < IN ? B_TR : A_TR) {
+      const unsigned at = o < IN ? at_b[B_TR ? idx : 0] : at_a[A_TR ? idx : 0];
+      f.lo[c] = lds_read_tr16_untracked<off + HALF * 4096>(at);
+      f.hi[c] = lds_read_tr16_untracked<off + HALF * 4096 + 512>(at);
+    } else {
+      f.full[c] = lds_read_b128_untracked<off + 2048 * idx>(o < IN ? at_b[HALF] : at_a[HALF]);
+    }
+  };
+  auto arrived = [&](Operands& f, int unit) __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<0, NS * OPS>([&](auto C_) __attribute__((always_inline)) {   // (one wait; the others only tie their registers to it)
+      constexpr int c = decltype(C_)::value;
+      if constexpr (c % OPS < IN ? B_TR : A_TR) {
+        if constexpr (c == 0) lds_wait<0>(f.lo[c], f.hi[c]);
+        else asm volatile("" : "+v"(f.lo[c]), "+v"(f.hi[c]));
+      } else {
+        if constexpr (c == 0) lds_wait<0>(f.full[c]);
+        else asm volatile("" : "+v"(f.full[c]));
+      }
+    });
+    // k past the share's end was repeated or is another share's: clear those slots, on both sides (infinities)
+    const int64_t left = k_own - G::kK * (int64_t)unit;
+    if (__builtin_expect(left < G::kK, 0)) {
+      static_for<0, NS * OPS>([&](auto C_) __attribute__((always_inline)) {
+        constexpr int c = decltype(C_)::value, k = c / OPS * kStep;
+        if constexpr (c % OPS < IN ? B_TR : A_TR) {
+#pragma unroll
+          for (int sl = 0; sl < 4; ++sl) {
+            if (k + 8 * gq + sl >= left) f.lo[c][sl] = 0;
+            if (k + 8 * gq + 4 + sl >= left) f.hi[c][sl] = 0;
+          }
+        } else {
+          if (k >= left) f.full[c] = bf16x8{0};   // (row form: K % 32 == 0)
+        }
+      });
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // The products of a unit; between the first half of them the next one's reads, and the requests of another
+  auto multiply = [&](Operands& f, Operands& next, bool more, auto LAST_) __attribute__((always_inline)) {
+    static_for<0, NS * NM>([&](auto I_) __attribute__((always_inline)) {
+      constexpr int i = decltype(I_)::value, h = i / NM, jn = i % IN, c = h * OPS + IN + i % NM / IN, cn = h * OPS + jn;
+      if constexpr (jn == 0 && A_TR) f.full[c] = join_tr(f.lo[c], f.hi[c]);
+      if constexpr (i % NM < IN && B_TR) f.full[cn] = join_tr(f.lo[cn], f.hi[cn]);
+      acc[jn][i % NM / IN] = mfma16(f.full[cn], f.full[c], acc[jn][i % NM / IN]);
+      if constexpr (!decltype(LAST_)::value) {
+        static_for<0, NS * OPS>([&](auto C_) __attribute__((always_inline)) {
+          if constexpr (decltype(C_)::value * NM / (2 * OPS) == i) read(C_, next);
+        });
+        constexpr int kPer = (G::kLoads + NS * NM - 1) / (NS * NM), q0 = i * kPer < G::kLoads ? i * kPer : G::kLoads;
+        if (more) static_for<q0, (q0 + kPer < G::kLoads ? q0 + kPer : G::kLoads)>(load);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    });
+  };
+  auto request = [&](int unit) __attribute__((always_inline)) {
+    begin(unit);
+    static_for<0, G::kLoads>(load);
+    end();
+  };
+  // waits until unit `unit` has landed: S - 1 units are requested behind unit `unit` - 1, none near the end
+  auto landed = [&](int unit) __attribute__((always_inline)) {
+    constexpr int kBehind = G::kLoads * (S - 2);
+    if (unit + S - 2 < units) __builtin_amdgcn_s_waitcnt(0x0F70 | (kBehind & 15) | ((kBehind >> 4) << 14));
+    else __builtin_amdgcn_s_waitcnt(0x0F70);
+  };
+
+  for (int i = 0; i < S - 1 && i < units; ++i) request(i);
+  landed(0);
+  __syncthreads();
+  static_for<0, NS * OPS>([&](auto C_) __attribute__((always_inline)) { read(C_, f0); });
+  if (S - 1 < units) request(S - 1);
+  arrived(f0, 0);
+  auto unit = [&](int j, Operands& f, Operands& next) __attribute__((always_inline)) {
+    // Unit j is in registers, and unit j + 1 has to have landed: behind it the ring's other S - 2 units are under way
+    landed(j + 1);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const bool more = j + S < units;
+    if (more) begin(j + S);
+    next_unit();
+    multiply(f, next, more, std::false_type{});
+    if (more) end();
+    arrived(next, j + 1);   // (here: no read may be under way where paths meet and registers are renamed)
+  };
+  auto last = [&](Operands& f) __attribute__((always_inline)) { multiply(f, f, false, std::true_type{}); };
+  int j = 0;
+  for (; j + 2 < units; j += 2) {
+    unit(j, f0, f1);
+    unit(j + 1, f1, f0);
+  }
+  if (j + 1 < units) {
+    unit(j, f0, f1);
+    last(f1);
+  } else {
+    last(f0);
+  }
+  __syncthreads();   // the ring is done with
+  if (sizeof(T) == 4) e.Y = static_cast<float*>(e.Y) + (int64_t)split * a.M * a.N;
+  wave_epilogue_by<T, IM / 2, IN / 2, sizeof(T) == 4>(
+      [&](auto IM_, unsigned char* piece) __attribute__((always_inline)) {
+        constexpr int im = decltype(IM_)::value;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int jn = 0; jn < IN; ++jn) put_sums<IN / 2>(piece, 16 * h + i16, 4 * jn + gq, acc[jn][2 * im + h]);
+      },
+      smem + wave * (32 * G::TN * 4), m0 + G::TM * wm, n0 + G::TN * wn, lane, e);
+}
+
+template <bool SMALL, bool A_TR, bool B_TR, typename G, typename T>
 int launch_tile(LinearGemmArgs a, const Epilogue& e, hipStream_t stream) {
-  using G = Tile<A_TR, B_TR, BM, BN, WM, WN>;
-  a.tiles_n = (a.N + BN - 1) / BN;
-  a.n_items = (a.M + BM - 1) / BM * a.tiles_n * a.splits;
-  if (hipError_t e0 = LdsLimit<&linear_gemm_kernel<A_TR, B_TR, G, T>, G::kLds>::ensure(); e0 != hipSuccess) return (int)e0;
-  hipLaunchKernelGGL((linear_gemm_kernel<A_TR, B_TR, G, T>), dim3((unsigned)xcd_grid_size(a.n_items)), dim3(512), G::kLds,
-                     stream, a, e);
+  a.tiles_n = (a.N + G::BN - 1) / G::BN;
+  a.n_items = (a.M + G::BM - 1) / G::BM * a.tiles_n * a.splits;
+  const dim3 grid((unsigned)xcd_grid_size(a.n_items));
+  if constexpr (SMALL) {
+    if (hipError_t e0 = LdsLimit<&linear_small_kernel<A_TR, B_TR, G, T>, G::kLds>::ensure(); e0 != hipSuccess) return (int)e0;
+    hipLaunchKernelGGL((linear_small_kernel<A_TR, B_TR, G, T>), grid, dim3(64 * G::NW), G::kLds, stream, a, e);
+  } else {
+    if (hipError_t e0 = LdsLimit<&linear_gemm_kernel<A_TR, B_TR, G, T>, G::kLds>::ensure(); e0 != hipSuccess) return (int)e0;
+    hipLaunchKernelGGL((linear_gemm_kernel<A_TR, B_TR, G, T>), grid, dim3(512), G::kLds, stream, a, e);
+  }
   return (int)hipGetLastError();
 }
 template <bool A_TR, bool B_TR, typename T>
-int launch_form(const LinearGemmArgs& a, const Epilogue& e, bool wide, hipStream_t stream) {
-  return wide ? launch_tile<A_TR, B_TR, 256, 256, 2, 4, T>(a, e, stream) : launch_tile<A_TR, B_TR, 256, 128, 4, 2, T>(a, e, stream);
+int launch_form(const LinearGemmArgs& a, const Epilogue& e, int shape, hipStream_t stream) {
+  switch (shape) {
+    case 0: return launch_tile<false, A_TR, B_TR, Tile<A_TR, B_TR, 256, 256, 2, 4>, T>(a, e, stream);
+    case 1: return launch_tile<false, A_TR, B_TR, Tile<A_TR, B_TR, 256, 128, 4, 2>, T>(a, e, stream);
+    case 2: return launch_tile<true, A_TR, B_TR, SmallTile<128, 128, 4, 1>, T>(a, e, stream);
+    case 3: return launch_tile<true, A_TR, B_TR, SmallTile<64, 128, 2, 1>, T>(a, e, stream);
+    default: return launch_tile<true, A_TR, B_TR, SmallTile<64, 64, 2, 2>, T>(a, e, stream);
+  }
 }
 template <typename T>
-int launch(bool a_tr, bool b_tr, const LinearGemmArgs& a, const Epilogue& e, bool wide, hipStream_t stream) {
-  if (!a_tr && b_tr) return launch_form<false, true, T>(a, e, wide, stream);
-  if (!a_tr && !b_tr) return launch_form<false, false, T>(a, e, wide, stream);
-  return a_tr && b_tr ? launch_form<true, true, T>(a, e, wide, stream) : -1;   // transposed A with row-form B: no caller
+int launch(bool a_tr, bool b_tr, const LinearGemmArgs& a, const Epilogue& e, int shape, hipStream_t stream) {
+  if (!a_tr && b_tr) return launch_form<false, true, T>(a, e, shape, stream);
+  if (!a_tr && !b_tr) return launch_form<false, false, T>(a, e, shape, stream);
+  return a_tr && b_tr ? launch_form<true, true, T>(a, e, shape, stream) : -1;   // transposed A with row-form B: no caller
+}
+
+// Tile shape and split of the contraction, by the time of the fullest CU.  Microseconds measured: a slice of k costs a
+// workgroup kSliceUs, what lies around its slices kAroundUs; the sum over the splits is a launch of 4.5 and moves
+// 5.7 MB a us.  The kernels for few rows: up to 16 (weights in row form: 8) 16 columns a workgroup, above 32 x 32.
+struct Plan { int shape, splits; int64_t slices_per_split; };   // shape -1: the kernels for few rows
+constexpr int kShapes = 5, kShapeM[kShapes] = {256, 256, 128, 64, 64}, kShapeN[kShapes] = {256, 128, 128, 128, 64};
+constexpr double kSliceUs[kShapes] = {0.74, 0.5, 0.3, 0.21, 0.14}, kAroundUs[kShapes] = {12, 5, 2.5, 1, 0.8};
+Plan plan_of(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K) {
+  const int64_t KT = (K + kStep - 1) / kStep;
+  Plan best{0, 1, KT};
+  double least = 0.0;
+  for (int sh = 0; sh < kShapes; ++sh) {
+    const int64_t tiles = ((M + kShapeM[sh] - 1) / kShapeM[sh]) * ((N + kShapeN[sh] - 1) / kShapeN[sh]);
+    for (int want = 1; want <= 16; ++want) {
+      const int64_t per = (KT + want - 1) / want;
+      if (want > 1 && (per < 8 || (KT + per - 1) / per != want)) continue;   // at least eight slices per workgroup
+      double cost = (double)((tiles * want + 255) / 256) * (per * kSliceUs[sh] + kAroundUs[sh]);
+      if (want > 1) cost += 4.5 + (double)want * M * N * 4 / 5.7e6;
+      if (least == 0.0 || cost < least) { least = cost; best = {sh, want, per}; }
+    }
+  }
+  if (!a_tr && N % 32 == 0 && K % 64 == 0) {
+    const bool few = M <= (b_tr ? 16 : 8);
+    const int64_t wgs = few ? N / 16 : (M + 31) / 32 * (N / 32);
+    if ((double)((wgs + 255) / 256) * (K / 64 * (few ? 0.12 : 0.2) + 0.7) < least) best = {-1, 1, KT};
+  }
+  return best;
 }
 
 }  // namespace
 
-int launch_linear_tiles(bool a_tr, bool b_tr, bool wide, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M,
-                        int64_t N, int64_t K, int splits, int64_t slices_per_split, const Epilogue& e, void* P, void* stream) {
-  LinearGemmArgs a = {static_cast<const uint16_t*>(A), static_cast<const uint16_t*>(B), M, N, K, lda, ldb, 0, 0, splits,
-                      slices_per_split};
+std::string linear_bf16_plan(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K) {
+  const Plan p = plan_of(a_tr, b_tr, M, N, K);
+  if (p.shape < 0) return "few rows";
+  return std::to_string(kShapeM[p.shape]) + "x" + std::to_string(kShapeN[p.shape]) + " splits=" + std::to_string(p.splits);
+}
+
+size_t linear_bf16_workspace_bytes(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K) {
+  const int splits = plan_of(a_tr, b_tr, M, N, K).splits;
+  return splits > 1 ? (size_t)splits * M * N * sizeof(float) : 0;
+}
+
+int launch_linear_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N,
+                       int64_t K, const Epilogue& e, void* ws, void* stream) {
+  const Plan p = plan_of(a_tr, b_tr, M, N, K);
+  if (p.shape < 0) return launch_linear_few_rows(b_tr, A, lda, B, ldb, M, N, K, e, stream);
+  LinearGemmArgs a = {static_cast<const uint16_t*>(A), static_cast<const uint16_t*>(B), M, N, K, lda, ldb, 0, 0, p.splits,
+                      p.slices_per_split};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (splits == 1) return launch<uint16_t>(a_tr, b_tr, a, with_vec(e, 1), wide, st);
+  if (p.splits == 1) return launch<uint16_t>(a_tr, b_tr, a, with_vec(e, 1), p.shape, st);
   Epilogue sums = {};
-  sums.Y = P; sums.ldy = N; sums.M = M; sums.N = N;   // (N % 8 == 0)
-  return launch<float>(a_tr, b_tr, a, with_vec(sums, 0), wide, st);
+  sums.Y = ws; sums.ldy = N; sums.M = M; sums.N = N;   // (N % 8 == 0)
+  const int rc = launch<float>(a_tr, b_tr, a, with_vec(sums, 0), p.shape, st);
+  return rc ? rc : launch_linear_epilogue(1, {static_cast<float*>(ws), N, p.splits}, e, stream);
 }
 
 }  // namespace mhffn

@@ -144,13 +144,12 @@ struct LinearSums {   // Epilogue over `splits` partial products P [splits][M][l
 // The product of the forms that launch_gemm_bf16 takes, followed by the epilogue: in the product's
 // kernel where it is not split, over its partial sums in `ws` otherwise.  N % 8 == 0 (e.N of the
 // columns exist); row-form operands hold K % 32 == 0.
-size_t linear_bf16_workspace_bytes(bool a_tr, int64_t M, int64_t N, int64_t K);
+size_t linear_bf16_workspace_bytes(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K);
 int launch_linear_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb,
                        int64_t M, int64_t N, int64_t K, const Epilogue& e, void* ws, void* stream);
-// Its large tiles, 256 x 256 (wide) or 256 x 128: the epilogue, or with splits > 1 the partial sums in P
-int launch_linear_tiles(bool a_tr, bool b_tr, bool wide, const void* A, int64_t lda, const void* B, int64_t ldb,
-                        int64_t M, int64_t N, int64_t K, int splits, int64_t slices_per_split,
-                        const Epilogue& e, void* P, void* stream);
+// Its kernels for a few rows (gemm_bf16.hip): N % 32 == 0, K % 64 == 0
+int launch_linear_few_rows(bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M,
+                           int64_t N, int64_t K, const Epilogue& e, void* stream);
 // The same in fp32: any sizes, any strides
 size_t linear_f32_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int launch_linear_f32(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M,
@@ -210,5 +209,8 @@ std::string gemm_bf16_plan(bool a_tr, int64_t M, int64_t N, int64_t K);
 // columns of C per workgroup of the few-rows kernel that an unaccumulated product takes (0: none)
 int gemm_bf16_few_columns(bool b_tr, int64_t M, int64_t N, int64_t K);
 std::string module_plan(const Problem& p, int dtype, bool backward);
+std::string linear_plan(const Linear& p, bool backward);
+std::string linear_bf16_plan(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K);
+std::string linear_f32_plan(int64_t M, int64_t N, int64_t K);
 
 }  // namespace mhffn
