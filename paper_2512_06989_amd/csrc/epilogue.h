@@ -132,56 +132,20 @@ __device__ __forceinline__ void slope8(float (&v)[8], const float (&z)[8], int a
 }
 
 // ---- pieces of eight columns in memory -----------------------------------------------------------
-// `cols`: how many of the eight exist; `vec`: rows are 16-byte aligned (a whole piece moves at once).
-__device__ __forceinline__ void unpack8(u32x4 w, float (&v)[8]) {
+// `cols`: how many of the eight exist (at least one).  A whole piece moves 16 bytes at a time wherever it lies: such
+// an access needs no more than its elements' alignment, and rows need none (an element at a time, fp32
+// rows of 1001 took twice the time).
+template <typename T> struct Raw8 { u32x4 w[sizeof(T) / 2]; };   // a piece as it lies in memory
+typedef uint32_t u32x4_any2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ void unpack8(const Raw8<uint16_t>& r, float (&v)[8]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    v[2 * j] = __builtin_bit_cast(float, w[j] << 16);
-    v[2 * j + 1] = __builtin_bit_cast(float, w[j] & 0xFFFF0000u);
+    const uint32_t two = r.w[0][j];
+    v[2 * j] = __builtin_bit_cast(float, two << 16);
+    v[2 * j + 1] = __builtin_bit_cast(float, two & 0xFFFF0000u);
   }
 }
-__device__ __forceinline__ void load8(const uint16_t* p, int cols, bool vec, float (&v)[8]) {
-  if (vec && cols >= 8) {
-    unpack8(*reinterpret_cast<const u32x4*>(p), v);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < cols ? bf16_bits_to_f32(p[j]) : 0.f;
-  }
-}
-__device__ __forceinline__ void load8(const float* p, int cols, bool vec, float (&v)[8]) {
-  if (vec && cols >= 8) {
-    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) { v[j] = a[j]; v[4 + j] = b[j]; }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < cols ? p[j] : 0.f;
-  }
-}
-__device__ __forceinline__ void store8(uint16_t* p, int cols, bool vec, const float (&v)[8]) {
-  const u32x4 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-  if (vec && cols >= 8) {
-    *reinterpret_cast<u32x4*>(p) = w;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < cols) p[j] = (uint16_t)(j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xFFFFu);
-  }
-}
-__device__ __forceinline__ void store8(float* p, int cols, bool vec, const float (&v)[8]) {
-  if (vec && cols >= 8) {
-    reinterpret_cast<f32x4*>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
-    reinterpret_cast<f32x4*>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < cols) p[j] = v[j];
-  }
-}
-
-// A piece as it lies in memory
-template <typename T> struct Raw8 { u32x4 w[sizeof(T) / 2]; };
-__device__ __forceinline__ void unpack8(const Raw8<uint16_t>& r, float (&v)[8]) { unpack8(r.w[0], v); }
 __device__ __forceinline__ void unpack8(const Raw8<float>& r, float (&v)[8]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -189,10 +153,19 @@ __device__ __forceinline__ void unpack8(const Raw8<float>& r, float (&v)[8]) {
     v[j] = __builtin_bit_cast(float, bits);
   }
 }
-__device__ __forceinline__ Raw8<uint16_t> load_raw8(const uint16_t* p, int cols, bool vec) {
+__device__ __forceinline__ Raw8<uint16_t> pack8(const float (&v)[8], uint16_t) {
+  return {{u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])}}};
+}
+__device__ __forceinline__ Raw8<float> pack8(const float (&v)[8], float) {
+  Raw8<float> r;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r.w[j >> 2][j & 3] = __builtin_bit_cast(uint32_t, v[j]);
+  return r;
+}
+__device__ __forceinline__ Raw8<uint16_t> load_raw8(const uint16_t* p, int cols) {
   Raw8<uint16_t> r;
-  if (vec && cols >= 8) {
-    r.w[0] = *reinterpret_cast<const u32x4*>(p);
+  if (cols >= 8) {
+    r.w[0] = *reinterpret_cast<const u32x4_any2*>(p);
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -200,17 +173,42 @@ __device__ __forceinline__ Raw8<uint16_t> load_raw8(const uint16_t* p, int cols,
   }
   return r;
 }
-__device__ __forceinline__ Raw8<float> load_raw8(const float* p, int cols, bool vec) {
+__device__ __forceinline__ Raw8<float> load_raw8(const float* p, int cols) {
   Raw8<float> r;
-  if (vec && cols >= 8) {
-    r.w[0] = reinterpret_cast<const u32x4*>(p)[0];
-    r.w[1] = reinterpret_cast<const u32x4*>(p)[1];
+  if (cols >= 8) {
+    r.w[0] = reinterpret_cast<const u32x4_any4*>(p)[0];
+    r.w[1] = reinterpret_cast<const u32x4_any4*>(p)[1];
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) r.w[j >> 2][j & 3] = j < cols ? __builtin_bit_cast(uint32_t, p[j]) : 0u;
   }
   return r;
 }
+__device__ __forceinline__ void store_raw8(uint16_t* p, int cols, const Raw8<uint16_t>& r) {
+  if (cols >= 8) {
+    *reinterpret_cast<u32x4_any2*>(p) = r.w[0];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < cols) p[j] = (uint16_t)(j & 1 ? r.w[0][j >> 1] >> 16 : r.w[0][j >> 1] & 0xFFFFu);
+  }
+}
+__device__ __forceinline__ void store_raw8(float* p, int cols, const Raw8<float>& r) {
+  if (cols >= 8) {
+    reinterpret_cast<u32x4_any4*>(p)[0] = r.w[0];
+    reinterpret_cast<u32x4_any4*>(p)[1] = r.w[1];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t bits = r.w[j >> 2][j & 3];
+      if (j < cols) p[j] = __builtin_bit_cast(float, bits);
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int cols, float (&v)[8]) { unpack8(load_raw8(p, cols), v); }
+template <typename T>
+__device__ __forceinline__ void store8(T* p, int cols, const float (&v)[8]) { store_raw8(p, cols, pack8(v, T{})); }
 
 // ---- the epilogue of pieces in one column of pieces -------------------------------------------------
 // Columns col .. col + 7 of any row, whose bias is read once.  residual() before finish(), by the
@@ -224,14 +222,14 @@ struct EpilogueColumns {
     cols = (int)(e.N - col < 8 ? e.N - col : 8);
 #pragma unroll
     for (int j = 0; j < 8; ++j) bias[j] = 0.f;
-    if (e.bias && cols > 0) load8(static_cast<const T*>(e.bias) + col, cols, true, bias);
+    if (e.bias && cols > 0) load8(static_cast<const T*>(e.bias) + col, cols, bias);
   }
   __device__ __forceinline__ Raw8<T> residual(int64_t row, const Epilogue& e) const {
-    if (e.residual && row < e.M && cols > 0) return load_raw8(static_cast<const T*>(e.residual) + row * e.ldr + col, cols, e.vec & 2);
+    if (e.residual && row < e.M && cols > 0) return load_raw8(static_cast<const T*>(e.residual) + row * e.ldr + col, cols);
     return Raw8<T>{};
   }
   __device__ __forceinline__ void store(const float (&v)[8], int64_t row, const Epilogue& e) const {
-    if (row < e.M && cols > 0) store8(static_cast<T*>(e.Y) + row * e.ldy + col, cols, e.vec & 4, v);
+    if (row < e.M && cols > 0) store8(static_cast<T*>(e.Y) + row * e.ldy + col, cols, v);
   }
   // v: the product's eight sums
   __device__ __forceinline__ void finish(float (&v)[8], int64_t row, const Raw8<T>& res, const Epilogue& e, const DropKey& key) const {
@@ -240,7 +238,7 @@ struct EpilogueColumns {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += bias[j];
     }
-    if (e.Z) store8(static_cast<T*>(e.Z) + row * e.ldz + col, cols, e.vec & 1, v);
+    if (e.Z) store8(static_cast<T*>(e.Z) + row * e.ldz + col, cols, v);
     activate8<T>(v, e.act);
     drop8(v, (uint64_t)row * (uint64_t)((e.N + 7) >> 3) + (uint64_t)(col >> 3), e.drop, key);
     if (e.residual) {
@@ -249,7 +247,7 @@ struct EpilogueColumns {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += r[j];
     }
-    store8(static_cast<T*>(e.Y) + row * e.ldy + col, cols, e.vec & 4, v);
+    store8(static_cast<T*>(e.Y) + row * e.ldy + col, cols, v);
   }
 };
 template <typename T>
@@ -325,35 +323,6 @@ __device__ __forceinline__ void wave_epilogue_by(Put&& put, unsigned char* piece
     __builtin_amdgcn_wave_barrier();
   }
 }
-// ... of products of 32 x 32: lane (r, g) holds columns 32 jn + 8 vq + 4 g + i of row 32 im + r in register 4 vq + i
-// of acc[jn][im]
-template <typename T, int IM, int IN>
-__device__ __forceinline__ void wave_epilogue(const f32x16 (&acc)[IN][IM], unsigned char* piece, int64_t m, int64_t n,
-                                              int lane, const Epilogue& e) {
-  const int r = lane & 31, g = lane >> 5;
-  wave_epilogue_by<T, IM, IN>(
-      [&](auto IM_, unsigned char* p) __attribute__((always_inline)) {
-        constexpr int im = decltype(IM_)::value;
-#pragma unroll
-        for (int jn = 0; jn < IN; ++jn)
-#pragma unroll
-          for (int vq = 0; vq < 4; ++vq)
-            put_sums<IN>(p, r, 8 * jn + 2 * vq + g,
-                         f32x4{acc[jn][im][4 * vq], acc[jn][im][4 * vq + 1], acc[jn][im][4 * vq + 2], acc[jn][im][4 * vq + 3]});
-      },
-      piece, m, n, lane, e);
-}
-
-// Host: which row tensors move whole pieces
-inline bool vec_rows(const void* p, int64_t ld, int dtype) {
-  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % (dtype == 1 ? 8 : 4) == 0;
-}
-inline Epilogue with_vec(Epilogue e, int dtype) {
-  e.vec = (vec_rows(e.Z, e.ldz, dtype) ? 1 : 0) | (vec_rows(e.residual, e.ldr, dtype) ? 2 : 0) |
-          (vec_rows(e.Y, e.ldy, dtype) ? 4 : 0);
-  return e;
-}
-
 // ---- division by a number that the host knows ----------------------------------------------------------
 // x / d for x < 2^32: m = ceil(2^64 / d) (d > 1), the product's upper 64 bits
 struct Divisor { uint32_t d, m_hi, m_lo; };

@@ -686,7 +686,7 @@ int launch_linear_few_rows(bool b_tr, const void* A, int64_t lda, const void* B,
   a.A = static_cast<const uint16_t*>(A);
   a.B = static_cast<const uint16_t*>(B);
   a.M = M; a.N = N; a.K = K; a.lda = lda; a.ldb = ldb;
-  return launch_few_rows(b_tr, a, with_vec(e, 1), static_cast<hipStream_t>(stream));
+  return launch_few_rows(b_tr, a, e, static_cast<hipStream_t>(stream));
 }
 
 }  // namespace mhffn

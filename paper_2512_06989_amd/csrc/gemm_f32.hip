@@ -4,13 +4,14 @@
 //
 // What bounds it: the fp32 matrix rate, 256 flop per clock and CU, a sixteenth of bf16's.  A slice of 32
 // k of a 128 x 128 tile is 4096 clocks of products against 32 KB to load and 64 KB of operands to
-// read from LDS, so loads go through registers (zeros past every edge, no alignment asked for), LDS
-// holds two slices, and one barrier separates them.
-// v_mfma_f32_32x32x2_f32: lane (r, g) holds row r (column r), k = g.  Step s of eight k takes k = 4 g + s of
-// both operands, so that a lane of a row-form operand reads its four steps at once.  n is on the
-// matrix row axis: a lane ends up with four consecutive n of one row m, as in the bf16 product.
-// LDS: row form [rows][32 + 4], transposed form [32 k][rows + 8] (the two halves of a wave, four k apart, lie 32
-// banks apart): no bank conflicts in either.
+// read from LDS, so loads go through registers (no alignment asked for; rows past an edge are repeated, k past the
+// end is zero), LDS holds two slices, and one barrier separates them.  The loads cost a seventh: 140 TFLOP/s without.
+// v_mfma_f32_16x16x4_f32: lane (i16, gq) holds row i16 (column i16), k = gq.  Step s of 16 k takes k = 4 gq + s of both
+// operands, so that a lane of a row-form operand reads its four steps at once.  n is on the matrix row axis:
+// a lane ends up with four consecutive n of one row m, as in the bf16 product.  (4096^3: 124
+// TFLOP/s, a library product 154; 2000 x 2048 x 768, 64 x 64 tiles: 61 us, 128 x 128 71.)
+// LDS: row form [rows][32], 16-byte chunks permuted by (row / 2) % 8; transposed form [32 k][rows + 4] (the quarters of
+// a wave, four k apart, lie 16 banks apart): no bank conflicts in either.
 #include "epilogue.h"
 
 #include <type_traits>
@@ -32,7 +33,7 @@ struct GemmF32Args {
 
 template <bool TR, int ROWS>
 struct OperandF32 {
-  static constexpr int kLd = TR ? ROWS + 8 : kFK + 4;
+  static constexpr int kLd = TR ? ROWS + 4 : kFK;
   static constexpr int kFloats = TR ? kFK * kLd : ROWS * kLd;
   static constexpr int kVecs = ROWS * kFK / 4 / kFThreads;   // 16-byte pieces per thread and slice
   // piece q of a thread: (row, k) of its first element
@@ -41,19 +42,40 @@ struct OperandF32 {
     if constexpr (TR) { k = i / (ROWS / 4); row = i % (ROWS / 4) * 4; }
     else { row = i / (kFK / 4); k = i % (kFK / 4) * 4; }
   }
-  // src: element (row 0 of the tile, k 0 of the slice); rows, ks: how many of each exist
-  static __device__ __forceinline__ void load(const float* src, int64_t ld, int64_t rows, int64_t ks, int tid, f32x4 (&v)[kVecs]) {
-    const bool whole = rows >= ROWS && ks >= kFK;
+  // Offsets of a thread's pieces from the tile's first element, in floats.  Rows past the edge repeat the last
+  // piece (their products are never stored).
+  static __device__ __forceinline__ void offsets(int64_t ld, int64_t rows, int tid, unsigned (&off)[kVecs]) {
 #pragma unroll
     for (int q = 0; q < kVecs; ++q) {
       int row, k;
       place(q, tid, row, k);
-      const float* p = TR ? src + k * ld + row : src + row * ld + k;
-      if (whole || (TR ? k < ks && row + 4 <= rows : row < rows && k + 4 <= ks)) {
-        v[q] = *reinterpret_cast<const f32x4_any*>(p);
-      } else {
+      const int64_t r = row < rows ? row : TR ? (rows - 1) & ~3 : rows - 1;
+      off[q] = (unsigned)(TR ? k * ld + r : r * ld + k);
+    }
+  }
+  // src: the tile's first element of this slice; rows, ks: how many rows and k of the slice exist
+  static __device__ __forceinline__ void load(const float* src, const unsigned (&off)[kVecs], int64_t rows, int64_t ks, int tid, f32x4 (&v)[kVecs]) {
+    const bool cut = TR && rows < ROWS && (rows & 3) != 0;   // the last piece of a k row is not whole
+    if (ks >= kFK && !cut) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[q][j] = (TR ? k < ks && row + j < rows : row < rows && k + j < ks) ? p[j] : 0.f;
+      for (int q = 0; q < kVecs; ++q) v[q] = *reinterpret_cast<const f32x4_any*>(src + off[q]);
+    } else if (ks >= kFK) {   // element by element, the last one repeated (no load waits for another)
+#pragma unroll
+      for (int q = 0; q < kVecs; ++q) {
+        int row, k;
+        place(q, tid, row, k);
+        row = row < rows ? row : (int)(rows - 1) & ~3;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[q][j] = src[off[q] + min(j, (int)rows - 1 - row)];
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < kVecs; ++q) {
+        int row, k;
+        place(q, tid, row, k);
+        if (TR) row = row < rows ? row : (int)(rows - 1) & ~3;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[q][j] = (TR ? k < ks && row + j < rows : k + j < ks) ? src[off[q] + j] : 0.f;
       }
     }
   }
@@ -62,31 +84,32 @@ struct OperandF32 {
     for (int q = 0; q < kVecs; ++q) {
       int row, k;
       place(q, tid, row, k);
-      *reinterpret_cast<f32x4*>(lds + (TR ? k * kLd + row : row * kLd + k)) = v[q];
+      *reinterpret_cast<f32x4*>(lds + (TR ? k * kLd + row : row * kLd + (k ^ (((row >> 1) & 7) << 2)))) = v[q];
     }
   }
-  // the four steps of k = 8 j .. 8 j + 7 of row `row`
-  static __device__ __forceinline__ f32x4 read(const float* lds, int row, int j, int g) {
+  // the four steps of k = 16 j .. 16 j + 15 of row `row`
+  static __device__ __forceinline__ f32x4 read(const float* lds, int row, int j, int gq) {
+    const int k = 16 * j + 4 * gq;
     if constexpr (TR) {
       f32x4 v;
 #pragma unroll
-      for (int s = 0; s < 4; ++s) v[s] = lds[(8 * j + 4 * g + s) * kLd + row];
+      for (int s = 0; s < 4; ++s) v[s] = lds[(k + s) * kLd + row];
       return v;
     } else {
-      return *reinterpret_cast<const f32x4*>(lds + row * kLd + 8 * j + 4 * g);
+      return *reinterpret_cast<const f32x4*>(lds + row * kLd + (k ^ (((row >> 1) & 7) << 2)));
     }
   }
 };
 
 template <bool A_TR, bool B_TR, int TILE>
 __global__ __launch_bounds__(kFThreads, 2) void gemm_f32_kernel(GemmF32Args a, Epilogue e) {
-  constexpr int W = TILE / 2, I = W / 32;     // four waves of W x W
+  constexpr int W = TILE / 2, I = W / 16;     // four waves of W x W
   using OA = OperandF32<A_TR, TILE>;
   using OB = OperandF32<B_TR, TILE>;
   constexpr int kStage = OA::kFloats + OB::kFloats;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   float* const lds = reinterpret_cast<float*>(smem);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, g = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i16 = lane & 15, gq = lane >> 4;
   const int64_t item = xcd_work_item(blockIdx.x, a.n_items);
   if (item >= a.n_items) return;
   const int split = (int)(item % a.splits);
@@ -94,18 +117,21 @@ __global__ __launch_bounds__(kFThreads, 2) void gemm_f32_kernel(GemmF32Args a, E
   const int64_t k0 = split * a.k_per_split, k1 = k0 + a.k_per_split < a.K ? k0 + a.k_per_split : a.K;
   const int wm = (wave >> 1) * W, wn = (wave & 1) * W;
 
-  f32x16 acc[I][I];
+  f32x4 acc[I][I];
 #pragma unroll
   for (int i = 0; i < I; ++i)
 #pragma unroll
-    for (int j = 0; j < I; ++j) acc[i][j] = f32x16{0};
+    for (int j = 0; j < I; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  f32x4 va[OA::kVecs], vb[OB::kVecs];
+  unsigned oa[OA::kVecs], ob[OB::kVecs];
+  OA::offsets(a.lda, a.M - m0, tid, oa);
+  OB::offsets(a.ldb, a.N - n0, tid, ob);
   const float* const pa = a.A + (A_TR ? m0 : m0 * a.lda);
   const float* const pb = a.B + (B_TR ? n0 : n0 * a.ldb);
+  f32x4 va[OA::kVecs], vb[OB::kVecs];
   auto load = [&](int64_t k) {
-    OA::load(pa + (A_TR ? k * a.lda : k), a.lda, a.M - m0, k1 - k, tid, va);
-    OB::load(pb + (B_TR ? k * a.ldb : k), a.ldb, a.N - n0, k1 - k, tid, vb);
+    OA::load(pa + (A_TR ? k * a.lda : k), oa, a.M - m0, k1 - k, tid, va);
+    OB::load(pb + (B_TR ? k * a.ldb : k), ob, a.N - n0, k1 - k, tid, vb);
   };
   auto store = [&](int stage) {
     OA::store(lds + stage * kStage, tid, va);
@@ -119,49 +145,61 @@ __global__ __launch_bounds__(kFThreads, 2) void gemm_f32_kernel(GemmF32Args a, E
     if (k + kFK < k1) load(k + kFK);
     const float* const la = lds + stage * kStage;
     const float* const lb = la + OA::kFloats;
+    stage ^= 1;
 #pragma unroll
-    for (int j = 0; j < kFK / 8; ++j) {
+    for (int j = 0; j < kFK / 16; ++j) {
       f32x4 fa[I], fb[I];
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        fa[i] = OA::read(la, wm + 32 * i + r, j, g);
-        fb[i] = OB::read(lb, wn + 32 * i + r, j, g);
+        fa[i] = OA::read(la, wm + 16 * i + i16, j, gq);
+        fb[i] = OB::read(lb, wn + 16 * i + i16, j, gq);
       }
 #pragma unroll
       for (int s = 0; s < 4; ++s)
 #pragma unroll
         for (int i = 0; i < I; ++i)
 #pragma unroll
-          for (int n = 0; n < I; ++n) acc[n][i] = __builtin_amdgcn_mfma_f32_32x32x2f32(fb[n][s], fa[i][s], acc[n][i], 0, 0, 0);
+          for (int n = 0; n < I; ++n)
+            acc[n][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[n][s], fa[i][s], acc[n][i], 0, 0, 0);
     }
-    stage ^= 1;
     if (k + kFK < k1) store(stage);
     __syncthreads();   // (everyone has read the slice that the next store overwrites)
   }
-  if (a.splits > 1) e.Y = static_cast<float*>(e.Y) + (int64_t)split * a.M * a.N;   // partial sums (16-byte aligned rows: N % 4 == 0)
-  wave_epilogue<float, I, I>(acc, smem + wave * (32 * W * 4), m0 + wm, n0 + wn, lane, e);
+  if (a.splits > 1) e.Y = static_cast<float*>(e.Y) + split * a.M * e.ldy;   // partial sums
+  wave_epilogue_by<float, I / 2, I / 2>(
+      [&](auto IM_, unsigned char* piece) __attribute__((always_inline)) {
+        constexpr int im = decltype(IM_)::value;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int jn = 0; jn < I; ++jn) put_sums<I / 2>(piece, 16 * h + i16, 4 * jn + gq, acc[jn][2 * im + h]);
+      },
+      smem + wave * (32 * W * 4), m0 + wm, n0 + wn, lane, e);
 }
 
-// Tile and split of the contraction: the workgroups of a CU share its matrix rate, so the time is
-// that of the fullest CU; clocks of a CU, measured around them 3000 a workgroup, and for the sum
-// over the splits 9000 and 2600 bytes a clock.
+// Tile and split of the contraction.  The workgroups of a CU share its matrix rate: with n of them a slice takes
+// kAlone + n kSlice microseconds (measured; what n hides is the latency of a slice), and 2 + n lie around the
+// slices; the sum over the splits is a launch of 6 and moves 5.7 MB a us.
 struct F32Plan { int tile, splits; int64_t k_per_split; };
 F32Plan plan_f32(int64_t M, int64_t N, int64_t K) {
   F32Plan best{128, 1, K};
   double least = 0.0;
   for (int tile : {128, 64}) {
+    const double kAlone = tile == 128 ? 1.02 : 0.42, kSlice = tile == 128 ? 1.88 : 0.53;
     const int64_t tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile);
     for (int want = 1; want <= 16; ++want) {
       const int64_t per = ((K + want - 1) / want + kFK - 1) / kFK * kFK;
       if (want > 1 && (per < 2 * kFK || (K + per - 1) / per != want)) continue;
-      const double slice = 2.0 * tile * tile * kFK / 256 * (tile == 128 ? 1.1 : 1.25);
-      double cost = (double)((tiles * want + 255) / 256) * ((double)((per + kFK - 1) / kFK) * slice + 3000);
-      if (want > 1) cost += 9000 + (double)want * M * N * 4 / 2600;
+      const double n = (double)((tiles * want + 255) / 256);
+      double cost = (double)((per + kFK - 1) / kFK) * (kAlone + kSlice * n) + 2 + n;
+      if (want > 1) cost += 6 + (double)want * M * N * 4 / 5.7e6;
       if (least == 0.0 || cost < least) { least = cost; best = {tile, want, per}; }
     }
   }
   return best;
 }
+
+int64_t partial_ld(int64_t N) { return (N + 3) & ~(int64_t)3; }   // rows of 16-byte pieces
 
 template <bool A_TR, bool B_TR, int TILE>
 int launch_tile(GemmF32Args a, const Epilogue& e, hipStream_t stream) {
@@ -191,7 +229,7 @@ std::string linear_f32_plan(int64_t M, int64_t N, int64_t K) {
 
 size_t linear_f32_workspace_bytes(int64_t M, int64_t N, int64_t K) {
   const int splits = plan_f32(M, N, K).splits;
-  return splits > 1 ? (size_t)splits * M * N * sizeof(float) : 0;
+  return splits > 1 ? (size_t)splits * M * partial_ld(N) * sizeof(float) : 0;
 }
 
 int launch_linear_f32(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N,
@@ -203,12 +241,11 @@ int launch_linear_f32(bool a_tr, bool b_tr, const void* A, int64_t lda, const vo
   Epilogue e = e0;
   if (plan.splits > 1) {
     e = {};
-    e.Y = ws; e.ldy = N; e.M = M; e.N = N;
+    e.Y = ws; e.ldy = partial_ld(N); e.M = M; e.N = N;
   }
-  e = with_vec(e, 0);
   const int rc = plan.tile == 128 ? launch_form<128>(a_tr, b_tr, a, e, st) : launch_form<64>(a_tr, b_tr, a, e, st);
   if (rc || plan.splits == 1) return rc;
-  return launch_linear_epilogue(0, {static_cast<float*>(ws), N, plan.splits}, e0, stream);
+  return launch_linear_epilogue(0, {static_cast<float*>(ws), partial_ld(N), plan.splits}, e0, stream);
 }
 
 }  // namespace mhffn

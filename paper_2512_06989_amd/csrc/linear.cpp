@@ -10,7 +10,7 @@ namespace {
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 size_t elt(int dtype) { return dtype == 1 ? 2 : 4; }
-constexpr int64_t kMostLd = 1 << 22;   // (gemm_bf16_supported)
+constexpr int64_t kMostLd = 1 << 22;   // (lane offsets inside a tile are 32-bit)
 
 // Workspace, handed out front to back; a null base only adds up
 struct Arena {
@@ -28,15 +28,14 @@ struct Operands {
   bool x, w, dz;          // packed X [M][Kp], packed W [Kp][Np], dZ [M][Np] in the workspace
   int64_t Kp, Np;
   Operands(const Linear& p, bool backward) {
-    Kp = up(p.K, 32);
-    Np = up(p.N, 32);
     const bool bf16 = p.dtype == 1;
-    const bool y_fits = p.ldy % 8 == 0 && p.ldy <= kMostLd;
-    x = bf16 && ((backward ? p.K % 8 : p.K % 32) != 0 || p.ldx % 8 != 0 || p.ldx > kMostLd);
+    Kp = bf16 ? up(p.K, 32) : p.K;
+    Np = bf16 ? up(p.N, 32) : p.N;
+    const bool y_fits = p.ldy <= kMostLd && (!bf16 || p.ldy % 8 == 0);
+    x = p.ldx > kMostLd || (bf16 && ((backward ? p.K % 8 : p.K % 32) != 0 || p.ldx % 8 != 0));
     w = bf16 && (backward ? p.K % 8 != 0 || p.N % 32 != 0 : p.K % 32 != 0 || p.N % 8 != 0);
-    dz = backward && (p.act != 0 || p.drop.threshold != 0 || (bf16 && (p.N % 32 != 0 || !y_fits)));
+    dz = backward && (p.act != 0 || p.drop.threshold != 0 || !y_fits || (bf16 && p.N % 32 != 0));
   }
-  int64_t ldz(const Linear& p) const { return p.dtype == 1 ? Np : p.N; }
 };
 
 size_t partial_bytes(int dtype, bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K) {
@@ -52,6 +51,13 @@ int product(int dtype, bool a_tr, bool b_tr, const void* A, int64_t lda, const v
 // Columns that the forward's product works on: with W packed its padding is there for the asking
 int64_t forward_columns(const Linear& p, const Operands& o) { return p.dtype != 1 ? p.N : o.w ? o.Np : up(p.N, 8); }
 
+PackJob pack_x(const Linear& p, const Operands& o, const void* X, void* Xp) {
+  return o.x ? PackJob{X, p.ldx, p.M, p.K, Xp, p.M, o.Kp} : PackJob{};
+}
+PackJob pack_w(const Linear& p, const Operands& o, const void* W, void* Wp) {
+  return o.w ? PackJob{W, p.N, p.K, p.N, Wp, o.Kp, o.Np} : PackJob{};
+}
+
 Epilogue plain(void* Y, int64_t ldy, int64_t M, int64_t N) {
   Epilogue e = {};
   e.Y = Y; e.ldy = ldy; e.M = M; e.N = N;
@@ -63,7 +69,7 @@ int forward(const Linear& p, const void* X, const void* W, const void* bias, con
   const Operands o(p, false);
   const bool bf16 = p.dtype == 1;
   Arena arena{static_cast<unsigned char*>(ws)};
-  void* const Xp = o.x ? arena.take((size_t)p.M * o.Kp * 2) : nullptr;
+  void* const Xp = o.x ? arena.take((size_t)p.M * o.Kp * elt(p.dtype)) : nullptr;
   void* const Wp = o.w ? arena.take((size_t)o.Kp * o.Np * 2) : nullptr;
   const int64_t K = bf16 && (o.x || o.w) ? o.Kp : p.K, N = forward_columns(p, o);
   float* const P = static_cast<float*>(arena.take(partial_bytes(p.dtype, false, true, p.M, N, K)));
@@ -71,9 +77,7 @@ int forward(const Linear& p, const void* X, const void* W, const void* bias, con
     *bytes = arena.used;
     return 0;
   }
-  int rc = 0;
-  if (o.x) rc = launch_pack(p.dtype, X, p.ldx, p.M, p.K, Xp, p.M, o.Kp, stream);
-  if (!rc && o.w) rc = launch_pack(p.dtype, W, p.N, p.K, p.N, Wp, o.Kp, o.Np, stream);
+  const int rc = launch_pack(p.dtype, pack_x(p, o, X, Xp), pack_w(p, o, W, Wp), stream);
   if (rc) return rc;
   Epilogue e = plain(Y, p.ldy, p.M, p.N);
   e.bias = bias;
@@ -90,13 +94,12 @@ int backward(const Linear& p, const void* X, const void* W, const void* Z, const
   const Operands o(p, true);
   const bool bf16 = p.dtype == 1;
   Arena arena{static_cast<unsigned char*>(ws)};
-  void* const Xp = o.x ? arena.take((size_t)p.M * o.Kp * 2) : nullptr;
+  void* const Xp = o.x ? arena.take((size_t)p.M * o.Kp * elt(p.dtype)) : nullptr;
   void* const Wp = o.w ? arena.take((size_t)o.Kp * o.Np * 2) : nullptr;
-  const int64_t ldz = o.ldz(p), K8 = bf16 ? up(p.K, 8) : p.K, N8 = bf16 ? up(p.N, 8) : p.N;
-  const int64_t Nk = bf16 ? o.Np : p.N;   // the contraction of dX
+  const int64_t ldz = o.Np, K8 = bf16 ? up(p.K, 8) : p.K, N8 = bf16 ? up(p.N, 8) : p.N;
   void* const dZ = o.dz ? arena.take((size_t)p.M * ldz * elt(p.dtype)) : nullptr;
   float* const sums = static_cast<float*>(arena.take((size_t)linear_column_blocks(p.M, p.N) * p.N * 4));
-  const size_t px = partial_bytes(p.dtype, false, false, p.M, K8, Nk), pw = partial_bytes(p.dtype, true, true, K8, N8, p.M);
+  const size_t px = partial_bytes(p.dtype, false, false, p.M, K8, o.Np), pw = partial_bytes(p.dtype, true, true, K8, N8, p.M);
   float* const P = static_cast<float*>(arena.take(px > pw ? px : pw));
   if (bytes) {
     *bytes = arena.used;
@@ -107,17 +110,16 @@ int backward(const Linear& p, const void* X, const void* W, const void* Z, const
   if (rc) return rc;
   const void* const G = o.dz ? dZ : dY;
   const int64_t ldg = o.dz ? ldz : p.ldy;
+  rc = launch_pack(p.dtype, dW ? pack_x(p, o, X, Xp) : PackJob{}, dX ? pack_w(p, o, W, Wp) : PackJob{}, stream);
+  if (rc) return rc;
   if (dX) {
-    if (o.w) rc = launch_pack(p.dtype, W, p.N, p.K, p.N, Wp, o.Kp, o.Np, stream);
-    if (!rc) rc = product(p.dtype, false, false, G, ldg, o.w ? Wp : W, o.w ? o.Np : p.N, p.M, K8, Nk, P,
+    rc = product(p.dtype, false, false, G, ldg, o.w ? Wp : W, o.w ? o.Np : p.N, p.M, K8, o.Np, P,
                           plain(dX, p.ldx, p.M, p.K), stream);
     if (rc) return rc;
   }
-  if (dW) {
-    if (o.x) rc = launch_pack(p.dtype, X, p.ldx, p.M, p.K, Xp, p.M, o.Kp, stream);
-    if (!rc) rc = product(p.dtype, true, true, o.x ? Xp : X, o.x ? o.Kp : p.ldx, G, ldg, K8, N8, p.M, P,
-                          plain(dW, p.N, p.K, p.N), stream);
-  }
+  if (dW)
+    rc = product(p.dtype, true, true, o.x ? Xp : X, o.x ? o.Kp : p.ldx, G, ldg, K8, N8, p.M, P, plain(dW, p.N, p.K, p.N),
+                 stream);
   return rc;
 }
 
@@ -154,9 +156,8 @@ int launch_linear_backward(const Linear& p, const void* X, const void* W, const 
                            void* dW, void* dbias, void* ws, void* stream) {
   if (p.M > 0) return backward(p, X, W, Z, dY, dX, dW, dbias, ws, nullptr, stream);
   // no rows: the parameters' gradients are zero
-  int rc = dW ? launch_pack(p.dtype, nullptr, 0, 0, 0, dW, p.K, p.N, stream) : 0;
-  if (!rc && dbias) rc = launch_pack(p.dtype, nullptr, 0, 0, 0, dbias, 1, p.N, stream);
-  return rc;
+  return launch_pack(p.dtype, dW ? PackJob{nullptr, 0, 0, 0, dW, p.K, p.N} : PackJob{},
+                     dbias ? PackJob{nullptr, 0, 0, 0, dbias, 1, p.N} : PackJob{}, stream);
 }
 
 }  // namespace mhffn

@@ -578,11 +578,11 @@ int launch(bool a_tr, bool b_tr, const LinearGemmArgs& a, const Epilogue& e, int
 }
 
 // Tile shape and split of the contraction, by the time of the fullest CU.  Microseconds measured: a slice of k costs a
-// workgroup kSliceUs, what lies around its slices kAroundUs; the sum over the splits is a launch of 4.5 and moves
+// workgroup kSliceUs, what lies around its slices kAroundUs; the sum over the splits is a launch of 6 and moves
 // 5.7 MB a us.  The kernels for few rows: up to 16 (weights in row form: 8) 16 columns a workgroup, above 32 x 32.
 struct Plan { int shape, splits; int64_t slices_per_split; };   // shape -1: the kernels for few rows
 constexpr int kShapes = 5, kShapeM[kShapes] = {256, 256, 128, 64, 64}, kShapeN[kShapes] = {256, 128, 128, 128, 64};
-constexpr double kSliceUs[kShapes] = {0.74, 0.5, 0.3, 0.21, 0.14}, kAroundUs[kShapes] = {12, 5, 2.5, 1, 0.8};
+constexpr double kSliceUs[kShapes] = {0.74, 0.5, 0.3, 0.21, 0.125}, kAroundUs[kShapes] = {12, 5, 2.5, 1, 1};
 Plan plan_of(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K) {
   const int64_t KT = (K + kStep - 1) / kStep;
   Plan best{0, 1, KT};
@@ -593,7 +593,7 @@ Plan plan_of(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K) {
       const int64_t per = (KT + want - 1) / want;
       if (want > 1 && (per < 8 || (KT + per - 1) / per != want)) continue;   // at least eight slices per workgroup
       double cost = (double)((tiles * want + 255) / 256) * (per * kSliceUs[sh] + kAroundUs[sh]);
-      if (want > 1) cost += 4.5 + (double)want * M * N * 4 / 5.7e6;
+      if (want > 1) cost += 6 + (double)want * M * N * 4 / 5.7e6;
       if (least == 0.0 || cost < least) { least = cost; best = {sh, want, per}; }
     }
   }
@@ -625,10 +625,10 @@ int launch_linear_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const v
   LinearGemmArgs a = {static_cast<const uint16_t*>(A), static_cast<const uint16_t*>(B), M, N, K, lda, ldb, 0, 0, p.splits,
                       p.slices_per_split};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (p.splits == 1) return launch<uint16_t>(a_tr, b_tr, a, with_vec(e, 1), p.shape, st);
+  if (p.splits == 1) return launch<uint16_t>(a_tr, b_tr, a, e, p.shape, st);
   Epilogue sums = {};
   sums.Y = ws; sums.ldy = N; sums.M = M; sums.N = N;   // (N % 8 == 0)
-  const int rc = launch<float>(a_tr, b_tr, a, with_vec(sums, 0), p.shape, st);
+  const int rc = launch<float>(a_tr, b_tr, a, sums, p.shape, st);
   return rc ? rc : launch_linear_epilogue(1, {static_cast<float*>(ws), N, p.splits}, e, stream);
 }
 

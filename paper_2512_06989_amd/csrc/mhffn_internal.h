@@ -118,7 +118,6 @@ struct Epilogue {
   void* Y;
   int64_t ldr, ldz, ldy, M, N;
   int act;               // mhffn_activation
-  int vec;               // bits: rows of Z (1), residual (2), Y (4) are 16-byte aligned
   Dropout drop;
 };
 struct Linear {
@@ -155,9 +154,14 @@ size_t linear_f32_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int launch_linear_f32(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M,
                       int64_t N, int64_t K, const Epilogue& e, void* ws, void* stream);
 int launch_linear_epilogue(int dtype, const LinearSums& s, const Epilogue& e, void* stream);
-// [rows][cols] (row stride ld) -> dense [rows_to][cols_to], zero outside
-int launch_pack(int dtype, const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst,
-                int64_t rows_to, int64_t cols_to, void* stream);
+// [rows][cols] (row stride ld) -> dense [rows_to][cols_to], zero outside; two at once (none: rows_to = 0)
+struct PackJob {
+  const void* src;
+  int64_t ld, rows, cols;
+  void* dst;
+  int64_t rows_to, cols_to;
+};
+int launch_pack(int dtype, const PackJob& a, const PackJob& b, void* stream);
 // dZ = D(dY) act'(Z) into dZ [M][ldz] (zero past column N; may be NULL), its column sums into
 // dbias (may be NULL) by way of `partials` (linear_column_blocks(M, N) x N floats)
 struct LinearDz {

@@ -16,15 +16,15 @@ struct Pieces {
 };
 Pieces make_pieces(int64_t rows, int64_t cols) {
   const uint32_t per = (uint32_t)((cols + 7) / 8);
-  return {rows * (int64_t)per, per, make_divisor(per)};
+  return {rows * (int64_t)per, per, make_divisor(per ? per : 1)};
 }
 __device__ __forceinline__ void piece_at(const Pieces& p, int64_t i, int64_t& row, int64_t& col) {
   row = p.total <= 0xFFFFFFFFll ? (int64_t)divide((uint32_t)i, p.div) : i / p.per_row;
   col = 8 * (i - row * p.per_row);
 }
 // (a launch holds fewer than 2^32 threads: past that a thread takes several pieces)
-unsigned piece_blocks(const Pieces& p) {
-  const int64_t blocks = (p.total + kThreads - 1) / kThreads;
+unsigned piece_blocks(int64_t pieces) {
+  const int64_t blocks = (pieces + kThreads - 1) / kThreads;
   return (unsigned)(blocks < (1 << 20) ? blocks : 1 << 20);
 }
 
@@ -36,10 +36,10 @@ __global__ __launch_bounds__(kThreads) void linear_epilogue_kernel(LinearSums s,
     piece_at(p, i, row, col);
     const int cols = (int)(s.ldp - col < 8 ? s.ldp - col : 8);
     float v[8];
-    load8(s.P + row * s.ldp + col, cols, (s.ldp & 3) == 0, v);
+    load8(s.P + row * s.ldp + col, cols, v);
     for (int k = 1; k < s.splits; ++k) {
       float w[8];
-      load8(s.P + ((int64_t)k * e.M + row) * s.ldp + col, cols, (s.ldp & 3) == 0, w);
+      load8(s.P + ((int64_t)k * e.M + row) * s.ldp + col, cols, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += w[j];
     }
@@ -48,26 +48,28 @@ __global__ __launch_bounds__(kThreads) void linear_epilogue_kernel(LinearSums s,
 }
 
 template <typename T>
-__global__ __launch_bounds__(kThreads) void dropout_kernel(const T* X, int64_t ldx, bool vec_x, Epilogue e, Pieces p) {
+__global__ __launch_bounds__(kThreads) void dropout_kernel(const T* X, int64_t ldx, Epilogue e, Pieces p) {
   const DropKey key = drop_key(e.drop);
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < p.total; i += (int64_t)gridDim.x * kThreads) {
     int64_t row, col;
     piece_at(p, i, row, col);
     float v[8];
-    load8(X + row * ldx + col, (int)(e.N - col < 8 ? e.N - col : 8), vec_x, v);
+    load8(X + row * ldx + col, (int)(e.N - col < 8 ? e.N - col : 8), v);
     epilogue8<T>(v, row, col, e, key);
   }
 }
 
+// One launch packs both operands of a product: pieces of the first, then of the second
 template <typename T>
-__global__ __launch_bounds__(kThreads) void pack_kernel(const T* src, int64_t ld, bool vec, int64_t rows, int64_t cols,
-                                                        T* dst, int64_t cols_to, Pieces p) {
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < p.total; i += (int64_t)gridDim.x * kThreads) {
+__global__ __launch_bounds__(kThreads) void pack_kernel(PackJob a, Pieces pa, PackJob b, Pieces pb) {
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < pa.total + pb.total; i += (int64_t)gridDim.x * kThreads) {
+    const bool first = i < pa.total;
+    const PackJob& j = first ? a : b;
     int64_t row, col;
-    piece_at(p, i, row, col);
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (row < rows && col < cols) load8(src + row * ld + col, (int)(cols - col < 8 ? cols - col : 8), vec, v);
-    store8(dst + row * cols_to + col, (int)(cols_to - col < 8 ? cols_to - col : 8), (cols_to & 7) == 0, v);
+    piece_at(first ? pa : pb, first ? i : i - pa.total, row, col);
+    Raw8<T> v = {};
+    if (row < j.rows && col < j.cols) v = load_raw8(static_cast<const T*>(j.src) + row * j.ld + col, (int)(j.cols - col < 8 ? j.cols - col : 8));
+    store_raw8(static_cast<T*>(j.dst) + row * j.cols_to + col, (int)(j.cols_to - col < 8 ? j.cols_to - col : 8), v);
   }
 }
 
@@ -80,7 +82,7 @@ struct DzGrid {
   int64_t rows_per_block;
 };
 template <typename T>
-__global__ __launch_bounds__(kThreads) void linear_dz_kernel(LinearDz a, DzGrid g, int vec) {
+__global__ __launch_bounds__(kThreads) void linear_dz_kernel(LinearDz a, DzGrid g) {
   __shared__ float sums[kThreads * 8];
   const DropKey key = drop_key(a.drop);
   const int lanes = 1 << g.lane_shift, at_once = kThreads >> g.lane_shift;
@@ -95,17 +97,17 @@ __global__ __launch_bounds__(kThreads) void linear_dz_kernel(LinearDz a, DzGrid 
     for (int64_t row = r0 + first; row < r1; row += at_once) {
       float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
       if (cols > 0) {
-        load8(static_cast<const T*>(a.dY) + row * a.ldy + col, cols, vec & 1, v);
+        load8(static_cast<const T*>(a.dY) + row * a.ldy + col, cols, v);
         drop8(v, (uint64_t)row * per_row + piece, a.drop, key);
         if (a.act) {
           float z[8];
-          load8(static_cast<const T*>(a.Z) + row * a.N + col, cols, vec & 2, z);
+          load8(static_cast<const T*>(a.Z) + row * a.N + col, cols, z);
           slope8<T>(v, z, a.act);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] += v[j];
       }
-      if (a.dZ) store8(static_cast<T*>(a.dZ) + row * a.ldz + col, (int)(a.ldz - col < 8 ? a.ldz - col : 8), vec & 4, v);
+      if (a.dZ) store8(static_cast<T*>(a.dZ) + row * a.ldz + col, (int)(a.ldz - col < 8 ? a.ldz - col : 8), v);
     }
   }
   if (!a.dbias) return;
@@ -158,43 +160,35 @@ int64_t linear_column_blocks(int64_t M, int64_t N) {
   return most < want ? (most > 0 ? most : 1) : want;
 }
 
-int launch_linear_epilogue(int dtype, const LinearSums& s, const Epilogue& e0, void* stream) {
-  const Epilogue e = with_vec(e0, dtype);
+int launch_linear_epilogue(int dtype, const LinearSums& s, const Epilogue& e, void* stream) {
   const Pieces p = make_pieces(e.M, e.N);
   if (p.total == 0) return 0;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dtype == 1) hipLaunchKernelGGL(linear_epilogue_kernel<uint16_t>, dim3(piece_blocks(p)), dim3(kThreads), 0, st, s, e, p);
-  else hipLaunchKernelGGL(linear_epilogue_kernel<float>, dim3(piece_blocks(p)), dim3(kThreads), 0, st, s, e, p);
+  if (dtype == 1) hipLaunchKernelGGL(linear_epilogue_kernel<uint16_t>, dim3(piece_blocks(p.total)), dim3(kThreads), 0, st, s, e, p);
+  else hipLaunchKernelGGL(linear_epilogue_kernel<float>, dim3(piece_blocks(p.total)), dim3(kThreads), 0, st, s, e, p);
   return (int)hipGetLastError();
 }
 
-int launch_dropout(int dtype, const void* X, int64_t ldx, const Epilogue& e0, void* stream) {
-  const Epilogue e = with_vec(e0, dtype);
+int launch_dropout(int dtype, const void* X, int64_t ldx, const Epilogue& e, void* stream) {
   const Pieces p = make_pieces(e.M, e.N);
   if (p.total == 0) return 0;
-  const bool vec = vec_rows(X, ldx, dtype);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dtype == 1)
-    hipLaunchKernelGGL(dropout_kernel<uint16_t>, dim3(piece_blocks(p)), dim3(kThreads), 0, st,
-                       static_cast<const uint16_t*>(X), ldx, vec, e, p);
+    hipLaunchKernelGGL(dropout_kernel<uint16_t>, dim3(piece_blocks(p.total)), dim3(kThreads), 0, st,
+                       static_cast<const uint16_t*>(X), ldx, e, p);
   else
-    hipLaunchKernelGGL(dropout_kernel<float>, dim3(piece_blocks(p)), dim3(kThreads), 0, st,
-                       static_cast<const float*>(X), ldx, vec, e, p);
+    hipLaunchKernelGGL(dropout_kernel<float>, dim3(piece_blocks(p.total)), dim3(kThreads), 0, st,
+                       static_cast<const float*>(X), ldx, e, p);
   return (int)hipGetLastError();
 }
 
-int launch_pack(int dtype, const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t rows_to,
-                int64_t cols_to, void* stream) {
-  const Pieces p = make_pieces(rows_to, cols_to);
-  if (p.total == 0) return 0;
-  const bool vec = vec_rows(src, ld, dtype);
+int launch_pack(int dtype, const PackJob& a, const PackJob& b, void* stream) {
+  const Pieces pa = make_pieces(a.rows_to, a.cols_to), pb = make_pieces(b.rows_to, b.cols_to);
+  if (pa.total + pb.total == 0) return 0;
+  const dim3 grid(piece_blocks(pa.total + pb.total));
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dtype == 1)
-    hipLaunchKernelGGL(pack_kernel<uint16_t>, dim3(piece_blocks(p)), dim3(kThreads), 0, st,
-                       static_cast<const uint16_t*>(src), ld, vec, rows, cols, static_cast<uint16_t*>(dst), cols_to, p);
-  else
-    hipLaunchKernelGGL(pack_kernel<float>, dim3(piece_blocks(p)), dim3(kThreads), 0, st,
-                       static_cast<const float*>(src), ld, vec, rows, cols, static_cast<float*>(dst), cols_to, p);
+  if (dtype == 1) hipLaunchKernelGGL(pack_kernel<uint16_t>, grid, dim3(kThreads), 0, st, a, pa, b, pb);
+  else hipLaunchKernelGGL(pack_kernel<float>, grid, dim3(kThreads), 0, st, a, pa, b, pb);
   return (int)hipGetLastError();
 }
 
@@ -202,13 +196,11 @@ int launch_linear_dz(int dtype, const LinearDz& a, void* stream) {
   if (!a.dZ && !a.dbias) return 0;
   const DzGrid g = dz_grid(a.M, a.N, a.dZ ? a.ldz : a.N);
   const int64_t blocks = linear_column_blocks(a.M, a.N);
-  const int vec = (vec_rows(a.dY, a.ldy, dtype) ? 1 : 0) | (vec_rows(a.Z, a.N, dtype) ? 2 : 0) |
-                  (vec_rows(a.dZ, a.ldz, dtype) ? 4 : 0);
   const dim3 grid((unsigned)((g.pieces + (1 << g.lane_shift) - 1) >> g.lane_shift), (unsigned)blocks);
   const dim3 sum_grid((unsigned)((a.N + 31) / 32));
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dtype == 1) hipLaunchKernelGGL(linear_dz_kernel<uint16_t>, grid, dim3(kThreads), 0, st, a, g, vec);
-  else hipLaunchKernelGGL(linear_dz_kernel<float>, grid, dim3(kThreads), 0, st, a, g, vec);
+  if (dtype == 1) hipLaunchKernelGGL(linear_dz_kernel<uint16_t>, grid, dim3(kThreads), 0, st, a, g);
+  else hipLaunchKernelGGL(linear_dz_kernel<float>, grid, dim3(kThreads), 0, st, a, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.dbias) return (int)e;
   if (dtype == 1)
