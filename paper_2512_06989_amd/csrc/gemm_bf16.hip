@@ -680,13 +680,12 @@ int launch_gemm_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const voi
   return -1;   // transposed A with row-form B: no caller
 }
 
-int launch_linear_few_rows(bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N, int64_t K,
-                           const Epilogue& e, void* stream) {
+int launch_linear_few_rows(const Product& p, void* stream) {
   TunedGemmArgs a = {};
-  a.A = static_cast<const uint16_t*>(A);
-  a.B = static_cast<const uint16_t*>(B);
-  a.M = M; a.N = N; a.K = K; a.lda = lda; a.ldb = ldb;
-  return launch_few_rows(b_tr, a, e, static_cast<hipStream_t>(stream));
+  a.A = static_cast<const uint16_t*>(p.A);
+  a.B = static_cast<const uint16_t*>(p.B);
+  a.M = p.M; a.N = p.N; a.K = p.K; a.lda = p.lda; a.ldb = p.ldb;
+  return launch_few_rows(p.b_tr, a, p.e, static_cast<hipStream_t>(stream));
 }
 
 }  // namespace mhffn

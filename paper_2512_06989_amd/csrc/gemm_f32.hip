@@ -102,16 +102,13 @@ struct OperandF32 {
 };
 
 template <bool A_TR, bool B_TR, int TILE>
-__global__ __launch_bounds__(kFThreads, 2) void gemm_f32_kernel(GemmF32Args a, Epilogue e) {
+__device__ __forceinline__ void gemm_f32_tile(const GemmF32Args& a, Epilogue e, int64_t item, unsigned char* smem) {
   constexpr int W = TILE / 2, I = W / 16;     // four waves of W x W
   using OA = OperandF32<A_TR, TILE>;
   using OB = OperandF32<B_TR, TILE>;
   constexpr int kStage = OA::kFloats + OB::kFloats;
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   float* const lds = reinterpret_cast<float*>(smem);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i16 = lane & 15, gq = lane >> 4;
-  const int64_t item = xcd_work_item(blockIdx.x, a.n_items);
-  if (item >= a.n_items) return;
   const int split = (int)(item % a.splits);
   const int64_t tile = item / a.splits, m0 = tile / a.tiles_n * TILE, n0 = tile % a.tiles_n * TILE;
   const int64_t k0 = split * a.k_per_split, k1 = k0 + a.k_per_split < a.K ? k0 + a.k_per_split : a.K;
@@ -177,23 +174,70 @@ __global__ __launch_bounds__(kFThreads, 2) void gemm_f32_kernel(GemmF32Args a, E
       smem + wave * (32 * W * 4), m0 + wm, n0 + wn, lane, e);
 }
 
+template <bool A_TR, bool B_TR, int TILE>
+__global__ __launch_bounds__(kFThreads, 2) void gemm_f32_kernel(GemmF32Args a, Epilogue e) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int64_t item = xcd_work_item(blockIdx.x, a.n_items);
+  if (item < a.n_items) gemm_f32_tile<A_TR, B_TR, TILE>(a, e, item, smem);
+}
+// Two products of a backward at once, dW (both transposed) and dX (both row form): neither fills the chip
+// with the three or four workgroups a CU that hide a slice's latency.
+constexpr int kPairTile = 64;
+__global__ __launch_bounds__(kFThreads, 2) void gemm_f32_pair_kernel(GemmF32Args w, Epilogue ew, GemmF32Args x, Epilogue ex, unsigned grid_w) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  if (blockIdx.x < grid_w) {
+    const int64_t item = xcd_work_item(blockIdx.x, w.n_items);
+    if (item < w.n_items) gemm_f32_tile<true, true, kPairTile>(w, ew, item, smem);
+  } else {
+    const int64_t item = xcd_work_item(blockIdx.x - grid_w, x.n_items);
+    if (item < x.n_items) gemm_f32_tile<false, false, kPairTile>(x, ex, item, smem);
+  }
+}
+
 // Tile and split of the contraction.  The workgroups of a CU share its matrix rate: with n of them a slice takes
 // kAlone + n kSlice microseconds (measured; what n hides is the latency of a slice), and 2 + n lie around the
 // slices; the sum over the splits is a launch of 6 and moves 5.7 MB a us.
-struct F32Plan { int tile, splits; int64_t k_per_split; };
+struct F32Plan { int tile, splits; int64_t k_per_split; double cost; };
+constexpr int kMostSplits = 16;
+constexpr double kAlone[2] = {1.02, 0.42}, kSlice[2] = {1.88, 0.53};   // of tiles of 128, 64
+int64_t tiles_of(int64_t M, int64_t N, int tile) { return ((M + tile - 1) / tile) * ((N + tile - 1) / tile); }
+// k of a share if `want` of them make sense, else 0
+int64_t share_of(int64_t K, int want) {
+  const int64_t per = ((K + want - 1) / want + kFK - 1) / kFK * kFK;
+  return want == 1 || (per >= 2 * kFK && (K + per - 1) / per == want) ? per : 0;
+}
+double sum_cost(int64_t M, int64_t N, int splits) { return splits > 1 ? 6 + (double)splits * M * N * 4 / 5.7e6 : 0; }
 F32Plan plan_f32(int64_t M, int64_t N, int64_t K) {
-  F32Plan best{128, 1, K};
-  double least = 0.0;
-  for (int tile : {128, 64}) {
-    const double kAlone = tile == 128 ? 1.02 : 0.42, kSlice = tile == 128 ? 1.88 : 0.53;
-    const int64_t tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile);
-    for (int want = 1; want <= 16; ++want) {
-      const int64_t per = ((K + want - 1) / want + kFK - 1) / kFK * kFK;
-      if (want > 1 && (per < 2 * kFK || (K + per - 1) / per != want)) continue;
+  F32Plan best{128, 1, K, 0.0};
+  for (int t = 0; t < 2; ++t) {
+    const int tile = 128 >> t;
+    const int64_t tiles = tiles_of(M, N, tile);
+    for (int want = 1; want <= kMostSplits; ++want) {
+      const int64_t per = share_of(K, want);
+      if (!per) continue;
       const double n = (double)((tiles * want + 255) / 256);
-      double cost = (double)((per + kFK - 1) / kFK) * (kAlone + kSlice * n) + 2 + n;
-      if (want > 1) cost += 6 + (double)want * M * N * 4 / 5.7e6;
-      if (least == 0.0 || cost < least) { least = cost; best = {tile, want, per}; }
+      const double cost = (double)(per / kFK) * (kAlone[t] + kSlice[t] * n) + 2 + n + sum_cost(M, N, want);
+      if (best.cost == 0.0 || cost < best.cost) best = {tile, want, per, cost};
+    }
+  }
+  return best;
+}
+// The two products of a backward in one launch, by the longest share and the mean of the slices of a CU
+struct F32Pair { bool worth; F32Plan x, w; };
+F32Pair plan_f32_pair(int64_t M, int64_t N, int64_t K) {   // the layer's sizes
+  const F32Plan x = plan_f32(M, K, N), w = plan_f32(K, N, M);
+  F32Pair best{false, x, w};
+  double least = x.cost + w.cost;
+  const int64_t tx = tiles_of(M, K, kPairTile), tw = tiles_of(K, N, kPairTile);
+  for (int sx = 1; sx <= kMostSplits; ++sx) {
+    const int64_t px = share_of(N, sx);
+    for (int sw = 1; px && sw <= kMostSplits; ++sw) {
+      const int64_t pw = share_of(M, sw);
+      if (!pw) continue;
+      const double longest = (double)((px > pw ? px : pw) / kFK), mean = (double)(tx * sx * px + tw * sw * pw) / kFK / 256;
+      const double cost = longest * kAlone[1] + (0.5 * longest + mean) * kSlice[1] + 2 + (double)(tx * sx + tw * sw) / 256 +
+                          sum_cost(M, K, sx) + sum_cost(K, N, sw);
+      if (cost < least) { least = cost; best = {true, {kPairTile, sx, px, cost}, {kPairTile, sw, pw, cost}}; }
     }
   }
   return best;
@@ -202,11 +246,13 @@ F32Plan plan_f32(int64_t M, int64_t N, int64_t K) {
 int64_t partial_ld(int64_t N) { return (N + 3) & ~(int64_t)3; }   // rows of 16-byte pieces
 
 template <bool A_TR, bool B_TR, int TILE>
-int launch_tile(GemmF32Args a, const Epilogue& e, hipStream_t stream) {
-  constexpr int kStages = 2 * (OperandF32<A_TR, TILE>::kFloats + OperandF32<B_TR, TILE>::kFloats) * 4;
-  constexpr int kOut = 4 * 32 * (TILE / 2) * 4, kLds = kStages > kOut ? kStages : kOut;
-  a.tiles_n = (a.N + TILE - 1) / TILE;
-  a.n_items = (a.M + TILE - 1) / TILE * a.tiles_n * a.splits;
+constexpr int lds_of() {
+  constexpr int kStages = 2 * (OperandF32<A_TR, TILE>::kFloats + OperandF32<B_TR, TILE>::kFloats) * 4, kOut = 4 * 32 * (TILE / 2) * 4;
+  return kStages > kOut ? kStages : kOut;
+}
+template <bool A_TR, bool B_TR, int TILE>
+int launch_tile(const GemmF32Args& a, const Epilogue& e, hipStream_t stream) {
+  constexpr int kLds = lds_of<A_TR, B_TR, TILE>();
   if (hipError_t e0 = LdsLimit<&gemm_f32_kernel<A_TR, B_TR, TILE>, kLds>::ensure(); e0 != hipSuccess) return (int)e0;
   hipLaunchKernelGGL((gemm_f32_kernel<A_TR, B_TR, TILE>), dim3((unsigned)xcd_grid_size(a.n_items)), dim3(kFThreads), kLds,
                      stream, a, e);
@@ -220,32 +266,67 @@ int launch_form(bool a_tr, bool b_tr, const GemmF32Args& a, const Epilogue& e, h
   return -1;   // transposed A with row-form B: no caller
 }
 
-}  // namespace
-
-std::string linear_f32_plan(int64_t M, int64_t N, int64_t K) {
-  const F32Plan p = plan_f32(M, N, K);
+size_t partials(int64_t M, int64_t N, const F32Plan& p) {
+  return p.splits > 1 ? (size_t)p.splits * M * partial_ld(N) * sizeof(float) : 0;
+}
+GemmF32Args args_of(const Product& p, const F32Plan& plan) {
+  const int64_t tiles_n = (p.N + plan.tile - 1) / plan.tile;
+  return {static_cast<const float*>(p.A), static_cast<const float*>(p.B), p.M, p.N, p.K, p.lda, p.ldb, tiles_n,
+          (p.M + plan.tile - 1) / plan.tile * tiles_n * plan.splits, plan.splits, plan.k_per_split};
+}
+Epilogue epilogue_of(const Product& p, const F32Plan& plan, void* ws) {
+  if (plan.splits == 1) return p.e;
+  Epilogue e = {};
+  e.Y = ws; e.ldy = partial_ld(p.N); e.M = p.M; e.N = p.N;
+  return e;
+}
+int sum_up(const Product& p, const F32Plan& plan, void* ws, void* stream) {
+  return plan.splits == 1 ? 0 : launch_linear_epilogue(0, {static_cast<float*>(ws), partial_ld(p.N), plan.splits}, p.e, stream);
+}
+std::string text_of(const F32Plan& p) {
   return std::to_string(p.tile) + "x" + std::to_string(p.tile) + " splits=" + std::to_string(p.splits);
 }
 
-size_t linear_f32_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-  const int splits = plan_f32(M, N, K).splits;
-  return splits > 1 ? (size_t)splits * M * partial_ld(N) * sizeof(float) : 0;
+}  // namespace
+
+std::string linear_f32_plan(int64_t M, int64_t N, int64_t K) { return text_of(plan_f32(M, N, K)); }
+std::string linear_f32_pair_plan(int64_t M, int64_t N, int64_t K) {
+  const F32Pair p = plan_f32_pair(M, N, K);
+  return "dX " + text_of(p.x) + (p.worth ? " with dW " : "; dW ") + text_of(p.w);
 }
 
-int launch_linear_f32(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N,
-                      int64_t K, const Epilogue& e0, void* ws, void* stream) {
-  const F32Plan plan = plan_f32(M, N, K);
-  GemmF32Args a = {static_cast<const float*>(A), static_cast<const float*>(B), M, N, K, lda, ldb, 0, 0, plan.splits,
-                   plan.k_per_split};
+size_t linear_f32_workspace_bytes(int64_t M, int64_t N, int64_t K) { return partials(M, N, plan_f32(M, N, K)); }
+size_t linear_f32_pair_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+  const F32Pair p = plan_f32_pair(M, N, K);
+  return partials(M, K, p.x) + partials(K, N, p.w);
+}
+
+int launch_linear_f32(const Product& p, void* ws, void* stream) {
+  const F32Plan plan = plan_f32(p.M, p.N, p.K);
+  const GemmF32Args a = args_of(p, plan);
+  const Epilogue e = epilogue_of(p, plan, ws);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  Epilogue e = e0;
-  if (plan.splits > 1) {
-    e = {};
-    e.Y = ws; e.ldy = partial_ld(N); e.M = M; e.N = N;
+  const int rc = plan.tile == 128 ? launch_form<128>(p.a_tr, p.b_tr, a, e, st) : launch_form<64>(p.a_tr, p.b_tr, a, e, st);
+  return rc ? rc : sum_up(p, plan, ws, stream);
+}
+
+int launch_linear_f32_pair(const Product& x, const Product& w, void* ws, void* stream) {
+  const F32Pair plan = plan_f32_pair(x.M, x.K, x.N);
+  void* const ws_w = static_cast<unsigned char*>(ws) + partials(x.M, x.N, plan.x);   // (x.M rows of 16-byte pieces)
+  int rc;
+  if (plan.worth) {
+    constexpr int kLds = lds_of<true, true, kPairTile>() > lds_of<false, false, kPairTile>() ? lds_of<true, true, kPairTile>() : lds_of<false, false, kPairTile>();
+    const GemmF32Args aw = args_of(w, plan.w), ax = args_of(x, plan.x);
+    const unsigned grid_w = (unsigned)xcd_grid_size(aw.n_items), grid_x = (unsigned)xcd_grid_size(ax.n_items);
+    if (hipError_t e0 = LdsLimit<&gemm_f32_pair_kernel, kLds>::ensure(); e0 != hipSuccess) return (int)e0;
+    hipLaunchKernelGGL(gemm_f32_pair_kernel, dim3(grid_w + grid_x), dim3(kFThreads), kLds, static_cast<hipStream_t>(stream), aw,
+                       epilogue_of(w, plan.w, ws_w), ax, epilogue_of(x, plan.x, ws), grid_w);
+    rc = (int)hipGetLastError();
+    if (!rc) rc = sum_up(x, plan.x, ws, stream);
+    return rc ? rc : sum_up(w, plan.w, ws_w, stream);
   }
-  const int rc = plan.tile == 128 ? launch_form<128>(a_tr, b_tr, a, e, st) : launch_form<64>(a_tr, b_tr, a, e, st);
-  if (rc || plan.splits == 1) return rc;
-  return launch_linear_epilogue(0, {static_cast<float*>(ws), partial_ld(N), plan.splits}, e0, stream);
+  rc = launch_linear_f32(x, ws, stream);
+  return rc ? rc : launch_linear_f32(w, ws_w, stream);
 }
 
 }  // namespace mhffn

@@ -42,12 +42,6 @@ size_t partial_bytes(int dtype, bool a_tr, bool b_tr, int64_t M, int64_t N, int6
   return dtype == 1 ? linear_bf16_workspace_bytes(a_tr, b_tr, M, N, K) : linear_f32_workspace_bytes(M, N, K);
 }
 
-// Epilogue e over A B
-int product(int dtype, bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M,
-            int64_t N, int64_t K, float* P, const Epilogue& e, void* stream) {
-  return (dtype == 1 ? launch_linear_bf16 : launch_linear_f32)(a_tr, b_tr, A, lda, B, ldb, M, N, K, e, P, stream);
-}
-
 // Columns that the forward's product works on: with W packed its padding is there for the asking
 int64_t forward_columns(const Linear& p, const Operands& o) { return p.dtype != 1 ? p.N : o.w ? o.Np : up(p.N, 8); }
 
@@ -72,7 +66,7 @@ int forward(const Linear& p, const void* X, const void* W, const void* bias, con
   void* const Xp = o.x ? arena.take((size_t)p.M * o.Kp * elt(p.dtype)) : nullptr;
   void* const Wp = o.w ? arena.take((size_t)o.Kp * o.Np * 2) : nullptr;
   const int64_t K = bf16 && (o.x || o.w) ? o.Kp : p.K, N = forward_columns(p, o);
-  float* const P = static_cast<float*>(arena.take(partial_bytes(p.dtype, false, true, p.M, N, K)));
+  void* const P = arena.take(partial_bytes(p.dtype, false, true, p.M, N, K));
   if (bytes) {
     *bytes = arena.used;
     return 0;
@@ -85,8 +79,8 @@ int forward(const Linear& p, const void* X, const void* W, const void* bias, con
   e.Z = Z; e.ldz = p.N;
   e.act = p.act;
   e.drop = p.drop;
-  return product(p.dtype, false, true, o.x ? Xp : X, o.x ? o.Kp : p.ldx, o.w ? Wp : W, o.w ? o.Np : p.N, p.M, N, K, P,
-                 e, stream);
+  const Product y = {false, true, o.x ? Xp : X, o.x ? o.Kp : p.ldx, o.w ? Wp : W, o.w ? o.Np : p.N, p.M, N, K, e};
+  return (bf16 ? launch_linear_bf16 : launch_linear_f32)(y, P, stream);
 }
 
 int backward(const Linear& p, const void* X, const void* W, const void* Z, const void* dY, void* dX, void* dW,
@@ -100,7 +94,8 @@ int backward(const Linear& p, const void* X, const void* W, const void* Z, const
   void* const dZ = o.dz ? arena.take((size_t)p.M * ldz * elt(p.dtype)) : nullptr;
   float* const sums = static_cast<float*>(arena.take((size_t)linear_column_blocks(p.M, p.N) * p.N * 4));
   const size_t px = partial_bytes(p.dtype, false, false, p.M, K8, o.Np), pw = partial_bytes(p.dtype, true, true, K8, N8, p.M);
-  float* const P = static_cast<float*>(arena.take(px > pw ? px : pw));
+  const size_t alone = px > pw ? px : pw, pair = bf16 ? 0 : linear_f32_pair_workspace_bytes(p.M, p.N, p.K);
+  void* const P = arena.take(alone > pair ? alone : pair);
   if (bytes) {
     *bytes = arena.used;
     return 0;
@@ -112,14 +107,12 @@ int backward(const Linear& p, const void* X, const void* W, const void* Z, const
   const int64_t ldg = o.dz ? ldz : p.ldy;
   rc = launch_pack(p.dtype, dW ? pack_x(p, o, X, Xp) : PackJob{}, dX ? pack_w(p, o, W, Wp) : PackJob{}, stream);
   if (rc) return rc;
-  if (dX) {
-    rc = product(p.dtype, false, false, G, ldg, o.w ? Wp : W, o.w ? o.Np : p.N, p.M, K8, o.Np, P,
-                          plain(dX, p.ldx, p.M, p.K), stream);
-    if (rc) return rc;
-  }
-  if (dW)
-    rc = product(p.dtype, true, true, o.x ? Xp : X, o.x ? o.Kp : p.ldx, G, ldg, K8, N8, p.M, P, plain(dW, p.N, p.K, p.N),
-                 stream);
+  const Product x = {false, false, G, ldg, o.w ? Wp : W, o.w ? o.Np : p.N, p.M, K8, o.Np, plain(dX, p.ldx, p.M, p.K)};
+  const Product w = {true, true, o.x ? Xp : X, o.x ? o.Kp : p.ldx, G, ldg, K8, N8, p.M, plain(dW, p.N, p.K, p.N)};
+  if (dX && dW && !bf16) return launch_linear_f32_pair(x, w, P, stream);
+  const auto launch = bf16 ? launch_linear_bf16 : launch_linear_f32;
+  if (dX) rc = launch(x, P, stream);
+  if (!rc && dW) rc = launch(w, P, stream);
   return rc;
 }
 
@@ -130,13 +123,10 @@ std::string linear_plan(const Linear& p, bool back) {
   std::string s = o.x ? "packed X " : "";
   if (o.w) s += "packed W ";
   if (o.dz) s += "dZ ";
-  auto plan = [&](bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K) {
-    return p.dtype == 1 ? linear_bf16_plan(a_tr, b_tr, M, N, K) : linear_f32_plan(M, N, K);
-  };
-  const bool bf16 = p.dtype == 1;
-  const int64_t K8 = bf16 ? up(p.K, 8) : p.K, N8 = bf16 ? up(p.N, 8) : p.N;
-  if (!back) return s + plan(false, true, p.M, forward_columns(p, o), o.x || o.w ? o.Kp : p.K);
-  return s + "dX " + plan(false, false, p.M, K8, bf16 ? o.Np : p.N) + "; dW " + plan(true, true, K8, N8, p.M);
+  if (p.dtype != 1) return s + (back ? linear_f32_pair_plan(p.M, p.N, p.K) : linear_f32_plan(p.M, p.N, p.K));
+  const int64_t K8 = up(p.K, 8), N8 = up(p.N, 8);
+  if (!back) return s + linear_bf16_plan(false, true, p.M, forward_columns(p, o), o.x || o.w ? o.Kp : p.K);
+  return s + "dX " + linear_bf16_plan(false, false, p.M, K8, o.Np) + "; dW " + linear_bf16_plan(true, true, K8, N8, p.M);
 }
 
 size_t linear_workspace_bytes(const Linear& p, bool back) {

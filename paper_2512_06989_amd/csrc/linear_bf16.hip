@@ -618,18 +618,17 @@ size_t linear_bf16_workspace_bytes(bool a_tr, bool b_tr, int64_t M, int64_t N, i
   return splits > 1 ? (size_t)splits * M * N * sizeof(float) : 0;
 }
 
-int launch_linear_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N,
-                       int64_t K, const Epilogue& e, void* ws, void* stream) {
-  const Plan p = plan_of(a_tr, b_tr, M, N, K);
-  if (p.shape < 0) return launch_linear_few_rows(b_tr, A, lda, B, ldb, M, N, K, e, stream);
-  LinearGemmArgs a = {static_cast<const uint16_t*>(A), static_cast<const uint16_t*>(B), M, N, K, lda, ldb, 0, 0, p.splits,
-                      p.slices_per_split};
+int launch_linear_bf16(const Product& p, void* ws, void* stream) {
+  const Plan plan = plan_of(p.a_tr, p.b_tr, p.M, p.N, p.K);
+  if (plan.shape < 0) return launch_linear_few_rows(p, stream);
+  LinearGemmArgs a = {static_cast<const uint16_t*>(p.A), static_cast<const uint16_t*>(p.B), p.M, p.N, p.K, p.lda, p.ldb, 0, 0,
+                      plan.splits, plan.slices_per_split};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (p.splits == 1) return launch<uint16_t>(a_tr, b_tr, a, e, p.shape, st);
+  if (plan.splits == 1) return launch<uint16_t>(p.a_tr, p.b_tr, a, p.e, plan.shape, st);
   Epilogue sums = {};
-  sums.Y = ws; sums.ldy = N; sums.M = M; sums.N = N;   // (N % 8 == 0)
-  const int rc = launch<float>(a_tr, b_tr, a, sums, p.shape, st);
-  return rc ? rc : launch_linear_epilogue(1, {static_cast<float*>(ws), N, p.splits}, e, stream);
+  sums.Y = ws; sums.ldy = p.N; sums.M = p.M; sums.N = p.N;   // (N % 8 == 0)
+  const int rc = launch<float>(p.a_tr, p.b_tr, a, sums, plan.shape, st);
+  return rc ? rc : launch_linear_epilogue(1, {static_cast<float*>(ws), p.N, plan.splits}, p.e, stream);
 }
 
 }  // namespace mhffn

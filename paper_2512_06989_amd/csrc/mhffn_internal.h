@@ -140,19 +140,27 @@ struct LinearSums {   // Epilogue over `splits` partial products P [splits][M][l
   int64_t ldp;
   int splits;
 };
-// The product of the forms that launch_gemm_bf16 takes, followed by the epilogue: in the product's
-// kernel where it is not split, over its partial sums in `ws` otherwise.  N % 8 == 0 (e.N of the
-// columns exist); row-form operands hold K % 32 == 0.
+// C[m][n] = sum_k A(m,k) B(n,k) of the forms that launch_gemm_bf16 takes, and its epilogue: in the product's
+// kernel where it is not split, over its partial sums in `ws` otherwise
+struct Product {
+  bool a_tr, b_tr;
+  const void* A;
+  int64_t lda;
+  const void* B;
+  int64_t ldb, M, N, K;
+  Epilogue e;
+};
+// bf16: N % 8 == 0 (e.N of the columns exist); row-form operands hold K % 32 == 0
 size_t linear_bf16_workspace_bytes(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K);
-int launch_linear_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb,
-                       int64_t M, int64_t N, int64_t K, const Epilogue& e, void* ws, void* stream);
+int launch_linear_bf16(const Product& p, void* ws, void* stream);
 // Its kernels for a few rows (gemm_bf16.hip): N % 32 == 0, K % 64 == 0
-int launch_linear_few_rows(bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M,
-                           int64_t N, int64_t K, const Epilogue& e, void* stream);
-// The same in fp32: any sizes, any strides
+int launch_linear_few_rows(const Product& p, void* stream);
+// fp32: any sizes, any strides.  The pair: dX [M][K] = dZ W^T and dW [K][N] = X^T dZ of a layer, in one launch where
+// that is worth it
 size_t linear_f32_workspace_bytes(int64_t M, int64_t N, int64_t K);
-int launch_linear_f32(bool a_tr, bool b_tr, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M,
-                      int64_t N, int64_t K, const Epilogue& e, void* ws, void* stream);
+int launch_linear_f32(const Product& p, void* ws, void* stream);
+size_t linear_f32_pair_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int launch_linear_f32_pair(const Product& dX, const Product& dW, void* ws, void* stream);
 int launch_linear_epilogue(int dtype, const LinearSums& s, const Epilogue& e, void* stream);
 // [rows][cols] (row stride ld) -> dense [rows_to][cols_to], zero outside; two at once (none: rows_to = 0)
 struct PackJob {
@@ -216,5 +224,6 @@ std::string module_plan(const Problem& p, int dtype, bool backward);
 std::string linear_plan(const Linear& p, bool backward);
 std::string linear_bf16_plan(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K);
 std::string linear_f32_plan(int64_t M, int64_t N, int64_t K);
+std::string linear_f32_pair_plan(int64_t M, int64_t N, int64_t K);
 
 }  // namespace mhffn
