@@ -323,6 +323,28 @@ __device__ __forceinline__ void wave_epilogue_by(Put&& put, unsigned char* piece
     __builtin_amdgcn_wave_barrier();
   }
 }
+// ---- sums of columns --------------------------------------------------------------------------------
+// 32 columns a workgroup of 256: thread (column t % 32, t / 32) adds up every eighth row, the eight sums meet
+// in LDS (one thread a column waited for each of its loads: 128 rows of 1024 columns took 31 us)
+constexpr int kSumThreads = 256;
+inline unsigned column_sum_blocks(const ColumnSums& c) { return c.blocks ? (unsigned)((c.N + 31) / 32) : 0; }
+template <typename T>
+__device__ __forceinline__ void column_sums(const ColumnSums& s, int64_t block, float* sums) {
+  const int64_t c = block * 32 + (threadIdx.x & 31);
+  float sum = 0.f;
+  if (c < s.N) {
+#pragma unroll 8
+    for (int64_t b = threadIdx.x >> 5; b < s.blocks; b += 8) sum += s.partials[b * s.N + c];
+  }
+  sums[threadIdx.x] = sum;
+  __syncthreads();
+  if (threadIdx.x >= 32 || c >= s.N) return;
+#pragma unroll
+  for (int k = 1; k < 8; ++k) sum += sums[32 * k + threadIdx.x];
+  if constexpr (sizeof(T) == 2) static_cast<uint16_t*>(s.out)[c] = (uint16_t)pack_bf16(sum, 0.f);
+  else static_cast<float*>(s.out)[c] = sum;
+}
+
 // ---- division by a number that the host knows ----------------------------------------------------------
 // x / d for x < 2^32: m = ceil(2^64 / d) (d > 1), the product's upper 64 bits
 struct Divisor { uint32_t d, m_hi, m_lo; };

@@ -280,8 +280,8 @@ Epilogue epilogue_of(const Product& p, const F32Plan& plan, void* ws) {
   e.Y = ws; e.ldy = partial_ld(p.N); e.M = p.M; e.N = p.N;
   return e;
 }
-int sum_up(const Product& p, const F32Plan& plan, void* ws, void* stream) {
-  return plan.splits == 1 ? 0 : launch_linear_epilogue(0, {static_cast<float*>(ws), partial_ld(p.N), plan.splits}, p.e, stream);
+LinearSums left_of(const Product& p, const F32Plan& plan, void* ws) {
+  return plan.splits == 1 ? LinearSums{} : LinearSums{static_cast<float*>(ws), partial_ld(p.N), plan.splits};
 }
 std::string text_of(const F32Plan& p) {
   return std::to_string(p.tile) + "x" + std::to_string(p.tile) + " splits=" + std::to_string(p.splits);
@@ -296,37 +296,34 @@ std::string linear_f32_pair_plan(int64_t M, int64_t N, int64_t K) {
 }
 
 size_t linear_f32_workspace_bytes(int64_t M, int64_t N, int64_t K) { return partials(M, N, plan_f32(M, N, K)); }
-size_t linear_f32_pair_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+bool linear_f32_pair(int64_t M, int64_t N, int64_t K, size_t& dX_bytes, size_t& dW_bytes) {
   const F32Pair p = plan_f32_pair(M, N, K);
-  return partials(M, K, p.x) + partials(K, N, p.w);
+  dX_bytes = partials(M, K, p.x);
+  dW_bytes = partials(K, N, p.w);
+  return p.worth;
 }
 
-int launch_linear_f32(const Product& p, void* ws, void* stream) {
+int launch_linear_f32(const Product& p, void* ws, LinearSums& left, void* stream) {
   const F32Plan plan = plan_f32(p.M, p.N, p.K);
   const GemmF32Args a = args_of(p, plan);
   const Epilogue e = epilogue_of(p, plan, ws);
+  left = left_of(p, plan, ws);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const int rc = plan.tile == 128 ? launch_form<128>(p.a_tr, p.b_tr, a, e, st) : launch_form<64>(p.a_tr, p.b_tr, a, e, st);
-  return rc ? rc : sum_up(p, plan, ws, stream);
+  return plan.tile == 128 ? launch_form<128>(p.a_tr, p.b_tr, a, e, st) : launch_form<64>(p.a_tr, p.b_tr, a, e, st);
 }
 
-int launch_linear_f32_pair(const Product& x, const Product& w, void* ws, void* stream) {
+int launch_linear_f32_pair(const Product& x, const Product& w, void* ws_x, void* ws_w, LinearSums& left_x, LinearSums& left_w,
+                           void* stream) {
+  constexpr int kLdsW = lds_of<true, true, kPairTile>(), kLdsX = lds_of<false, false, kPairTile>(), kLds = kLdsW > kLdsX ? kLdsW : kLdsX;
   const F32Pair plan = plan_f32_pair(x.M, x.K, x.N);
-  void* const ws_w = static_cast<unsigned char*>(ws) + partials(x.M, x.N, plan.x);   // (x.M rows of 16-byte pieces)
-  int rc;
-  if (plan.worth) {
-    constexpr int kLds = lds_of<true, true, kPairTile>() > lds_of<false, false, kPairTile>() ? lds_of<true, true, kPairTile>() : lds_of<false, false, kPairTile>();
-    const GemmF32Args aw = args_of(w, plan.w), ax = args_of(x, plan.x);
-    const unsigned grid_w = (unsigned)xcd_grid_size(aw.n_items), grid_x = (unsigned)xcd_grid_size(ax.n_items);
-    if (hipError_t e0 = LdsLimit<&gemm_f32_pair_kernel, kLds>::ensure(); e0 != hipSuccess) return (int)e0;
-    hipLaunchKernelGGL(gemm_f32_pair_kernel, dim3(grid_w + grid_x), dim3(kFThreads), kLds, static_cast<hipStream_t>(stream), aw,
-                       epilogue_of(w, plan.w, ws_w), ax, epilogue_of(x, plan.x, ws), grid_w);
-    rc = (int)hipGetLastError();
-    if (!rc) rc = sum_up(x, plan.x, ws, stream);
-    return rc ? rc : sum_up(w, plan.w, ws_w, stream);
-  }
-  rc = launch_linear_f32(x, ws, stream);
-  return rc ? rc : launch_linear_f32(w, ws_w, stream);
+  const GemmF32Args aw = args_of(w, plan.w), ax = args_of(x, plan.x);
+  const unsigned grid_w = (unsigned)xcd_grid_size(aw.n_items), grid_x = (unsigned)xcd_grid_size(ax.n_items);
+  left_x = left_of(x, plan.x, ws_x);
+  left_w = left_of(w, plan.w, ws_w);
+  if (hipError_t e0 = LdsLimit<&gemm_f32_pair_kernel, kLds>::ensure(); e0 != hipSuccess) return (int)e0;
+  hipLaunchKernelGGL(gemm_f32_pair_kernel, dim3(grid_w + grid_x), dim3(kFThreads), kLds, static_cast<hipStream_t>(stream), aw,
+                     epilogue_of(w, plan.w, ws_w), ax, epilogue_of(x, plan.x, ws_x), grid_w);
+  return (int)hipGetLastError();
 }
 
 }  // namespace mhffn

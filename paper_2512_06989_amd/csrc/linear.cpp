@@ -71,7 +71,7 @@ int forward(const Linear& p, const void* X, const void* W, const void* bias, con
     *bytes = arena.used;
     return 0;
   }
-  const int rc = launch_pack(p.dtype, pack_x(p, o, X, Xp), pack_w(p, o, W, Wp), stream);
+  int rc = launch_pack(p.dtype, pack_x(p, o, X, Xp), pack_w(p, o, W, Wp), stream);
   if (rc) return rc;
   Epilogue e = plain(Y, p.ldy, p.M, p.N);
   e.bias = bias;
@@ -80,7 +80,9 @@ int forward(const Linear& p, const void* X, const void* W, const void* bias, con
   e.act = p.act;
   e.drop = p.drop;
   const Product y = {false, true, o.x ? Xp : X, o.x ? o.Kp : p.ldx, o.w ? Wp : W, o.w ? o.Np : p.N, p.M, N, K, e};
-  return (bf16 ? launch_linear_bf16 : launch_linear_f32)(y, P, stream);
+  LinearSums left;
+  rc = (bf16 ? launch_linear_bf16 : launch_linear_f32)(y, P, left, stream);
+  return rc ? rc : launch_linear_sums(p.dtype, left, e, {}, {}, {}, stream);
 }
 
 int backward(const Linear& p, const void* X, const void* W, const void* Z, const void* dY, void* dX, void* dW,
@@ -93,15 +95,20 @@ int backward(const Linear& p, const void* X, const void* W, const void* Z, const
   const int64_t ldz = o.Np, K8 = bf16 ? up(p.K, 8) : p.K, N8 = bf16 ? up(p.N, 8) : p.N;
   void* const dZ = o.dz ? arena.take((size_t)p.M * ldz * elt(p.dtype)) : nullptr;
   float* const sums = static_cast<float*>(arena.take((size_t)linear_column_blocks(p.M, p.N) * p.N * 4));
-  const size_t px = partial_bytes(p.dtype, false, false, p.M, K8, o.Np), pw = partial_bytes(p.dtype, true, true, K8, N8, p.M);
-  const size_t alone = px > pw ? px : pw, pair = bf16 ? 0 : linear_f32_pair_workspace_bytes(p.M, p.N, p.K);
-  void* const P = arena.take(alone > pair ? alone : pair);
+  // Both products at once, or one after the other; what is split is added up at the end
+  size_t px, pw;
+  const bool pair = bf16 ? linear_bf16_pair(p.M, N8, K8, o.Np) : linear_f32_pair(p.M, p.N, p.K, px, pw);
+  const size_t ax = partial_bytes(p.dtype, false, false, p.M, K8, o.Np), aw = partial_bytes(p.dtype, true, true, K8, N8, p.M);
+  if (bf16 || !pair) px = pw = 0;
+  void* const Px = arena.take(ax > px ? ax : px);
+  void* const Pw = arena.take(aw > pw ? aw : pw);
   if (bytes) {
     *bytes = arena.used;
     return 0;
   }
   LinearDz z = {dY, Z, dX || dW ? dZ : nullptr, dbias, sums, p.M, p.N, p.ldy, ldz, p.act, p.drop};
-  int rc = launch_linear_dz(p.dtype, z, stream);
+  ColumnSums columns;
+  int rc = launch_linear_dz(p.dtype, z, columns, stream);
   if (rc) return rc;
   const void* const G = o.dz ? dZ : dY;
   const int64_t ldg = o.dz ? ldz : p.ldy;
@@ -109,11 +116,16 @@ int backward(const Linear& p, const void* X, const void* W, const void* Z, const
   if (rc) return rc;
   const Product x = {false, false, G, ldg, o.w ? Wp : W, o.w ? o.Np : p.N, p.M, K8, o.Np, plain(dX, p.ldx, p.M, p.K)};
   const Product w = {true, true, o.x ? Xp : X, o.x ? o.Kp : p.ldx, G, ldg, K8, N8, p.M, plain(dW, p.N, p.K, p.N)};
-  if (dX && dW && !bf16) return launch_linear_f32_pair(x, w, P, stream);
-  const auto launch = bf16 ? launch_linear_bf16 : launch_linear_f32;
-  if (dX) rc = launch(x, P, stream);
-  if (!rc && dW) rc = launch(w, P, stream);
-  return rc;
+  LinearSums left_x = {}, left_w = {};
+  if (dX && dW && pair) {
+    if (bf16) return launch_linear_bf16_pair(x, w, columns, stream);
+    rc = launch_linear_f32_pair(x, w, Px, Pw, left_x, left_w, stream);
+  } else {
+    const auto launch = bf16 ? launch_linear_bf16 : launch_linear_f32;
+    if (dX) rc = launch(x, Px, left_x, stream);
+    if (!rc && dW) rc = launch(w, Pw, left_w, stream);
+  }
+  return rc ? rc : launch_linear_sums(p.dtype, left_x, x.e, left_w, w.e, columns, stream);
 }
 
 }  // namespace
@@ -126,7 +138,7 @@ std::string linear_plan(const Linear& p, bool back) {
   if (p.dtype != 1) return s + (back ? linear_f32_pair_plan(p.M, p.N, p.K) : linear_f32_plan(p.M, p.N, p.K));
   const int64_t K8 = up(p.K, 8), N8 = up(p.N, 8);
   if (!back) return s + linear_bf16_plan(false, true, p.M, forward_columns(p, o), o.x || o.w ? o.Kp : p.K);
-  return s + "dX " + linear_bf16_plan(false, false, p.M, K8, o.Np) + "; dW " + linear_bf16_plan(true, true, K8, N8, p.M);
+  return s + "dX " + linear_bf16_plan(false, false, p.M, K8, o.Np) + (linear_bf16_pair(p.M, N8, K8, o.Np) ? " with dW " : "; dW ") + linear_bf16_plan(true, true, K8, N8, p.M);
 }
 
 size_t linear_workspace_bytes(const Linear& p, bool back) {

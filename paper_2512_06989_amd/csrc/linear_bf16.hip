@@ -87,8 +87,8 @@ __device__ __forceinline__ int tr_flip(int kr) { return (kr & 2) | ((kr >> 1) & 
 // of kBand tiles along n: the 32 workgroups that run at once there form a patch of about 4 x 8 tiles, whose 12
 // panels meet in its L2.
 template <typename G>
-__device__ __forceinline__ bool place_of(const LinearGemmArgs& a, int64_t& m0, int64_t& n0, int& split, int64_t& kbase, int64_t& kend) {
-  const int64_t item = xcd_work_item(blockIdx.x, a.n_items);
+__device__ __forceinline__ bool place_of(const LinearGemmArgs& a, int64_t block, int64_t& m0, int64_t& n0, int& split, int64_t& kbase, int64_t& kend) {
+  const int64_t item = xcd_work_item(block, a.n_items);
   if (item >= a.n_items) return false;
   const uint32_t n_tiles = (uint32_t)(a.n_items / a.splits), t = (uint32_t)(item % n_tiles);
   split = (int)(item / n_tiles);
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(512, 2) void linear_gemm_kernel(LinearGemmArgs a, E
   const bool late = wave >= 4;
   int64_t m0, n0, kbase, kend;   // tile, slices of k
   int split;
-  if (!place_of<G>(a, m0, n0, split, kbase, kend)) return;
+  if (!place_of<G>(a, blockIdx.x, m0, n0, split, kbase, kend)) return;
   const int64_t K = a.K, KT_all = (K + kStep - 1) / kStep;
   const int KT = (int)(kend - kbase);                         // its number of slices (>= 1)
 
@@ -335,15 +335,14 @@ struct SmallTile {
 };
 
 template <bool A_TR, bool B_TR, typename G, typename T>
-__global__ __launch_bounds__(64 * G::NW, G::NW / 4) void linear_small_kernel(LinearGemmArgs a, Epilogue e) {
+__device__ __forceinline__ void linear_small_tile(const LinearGemmArgs& a, Epilogue e, int64_t block, unsigned char* smem) {
   constexpr int IM = G::IM, IN = G::IN, OPS = IM + IN, NM = IM * IN, S = G::kSlots, NS = 2 * G::NK;   // operands and products of 32 k, of which a unit has NS
-  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i16 = lane & 15, gq = lane >> 4;
   const int wm = wave / G::WN, wn = wave % G::WN;
   int64_t m0, n0, kbase, kend;
   int split;
-  if (!place_of<G>(a, m0, n0, split, kbase, kend)) return;
+  if (!place_of<G>(a, block, m0, n0, split, kbase, kend)) return;
   const int64_t K = a.K, k0 = kbase * kStep, k_own = (kend * kStep < K ? kend * kStep : K) - k0;
   const int units = (int)((kend - kbase + NS - 1) / NS);
 
@@ -546,11 +545,31 @@ __global__ __launch_bounds__(64 * G::NW, G::NW / 4) void linear_small_kernel(Lin
       smem + wave * (32 * G::TN * 4), m0 + G::TM * wm, n0 + G::TN * wn, lane, e);
 }
 
-template <bool SMALL, bool A_TR, bool B_TR, typename G, typename T>
-int launch_tile(LinearGemmArgs a, const Epilogue& e, hipStream_t stream) {
+template <bool A_TR, bool B_TR, typename G, typename T>
+__global__ __launch_bounds__(64 * G::NW, G::NW / 4) void linear_small_kernel(LinearGemmArgs a, Epilogue e) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  linear_small_tile<A_TR, B_TR, G, T>(a, e, blockIdx.x, smem);
+}
+// A backward of few tiles: dW, dX and dbias in one launch
+using PairTile = SmallTile<64, 64, 2, 2>;
+__global__ __launch_bounds__(64 * PairTile::NW, PairTile::NW / 4) void linear_pair_kernel(LinearGemmArgs w, Epilogue ew, LinearGemmArgs x, Epilogue ex,
+                                                                                     ColumnSums c, unsigned grid_w, unsigned grid_x) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  static_assert(64 * PairTile::NW == kSumThreads, "");
+  if (blockIdx.x < grid_w) linear_small_tile<true, true, PairTile, uint16_t>(w, ew, blockIdx.x, smem);
+  else if (blockIdx.x < grid_w + grid_x) linear_small_tile<false, false, PairTile, uint16_t>(x, ex, blockIdx.x - grid_w, smem);
+  else column_sums<uint16_t>(c, blockIdx.x - grid_w - grid_x, reinterpret_cast<float*>(smem));
+}
+
+template <typename G>
+unsigned set_tiles(LinearGemmArgs& a) {   // returns the grid
   a.tiles_n = (a.N + G::BN - 1) / G::BN;
   a.n_items = (a.M + G::BM - 1) / G::BM * a.tiles_n * a.splits;
-  const dim3 grid((unsigned)xcd_grid_size(a.n_items));
+  return (unsigned)xcd_grid_size(a.n_items);
+}
+template <bool SMALL, bool A_TR, bool B_TR, typename G, typename T>
+int launch_tile(LinearGemmArgs a, const Epilogue& e, hipStream_t stream) {
+  const dim3 grid(set_tiles<G>(a));
   if constexpr (SMALL) {
     if (hipError_t e0 = LdsLimit<&linear_small_kernel<A_TR, B_TR, G, T>, G::kLds>::ensure(); e0 != hipSuccess) return (int)e0;
     hipLaunchKernelGGL((linear_small_kernel<A_TR, B_TR, G, T>), grid, dim3(64 * G::NW), G::kLds, stream, a, e);
@@ -567,7 +586,7 @@ int launch_form(const LinearGemmArgs& a, const Epilogue& e, int shape, hipStream
     case 1: return launch_tile<false, A_TR, B_TR, Tile<A_TR, B_TR, 256, 128, 4, 2>, T>(a, e, stream);
     case 2: return launch_tile<true, A_TR, B_TR, SmallTile<128, 128, 4, 1>, T>(a, e, stream);
     case 3: return launch_tile<true, A_TR, B_TR, SmallTile<64, 128, 2, 1>, T>(a, e, stream);
-    default: return launch_tile<true, A_TR, B_TR, SmallTile<64, 64, 2, 2>, T>(a, e, stream);
+    default: return launch_tile<true, A_TR, B_TR, PairTile, T>(a, e, stream);
   }
 }
 template <typename T>
@@ -604,6 +623,10 @@ Plan plan_of(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K) {
   }
   return best;
 }
+LinearGemmArgs args_of(const Product& p, const Plan& plan) {
+  return {static_cast<const uint16_t*>(p.A), static_cast<const uint16_t*>(p.B), p.M, p.N, p.K, p.lda, p.ldb, 0, 0, plan.splits,
+          plan.slices_per_split};
+}
 
 }  // namespace
 
@@ -618,17 +641,31 @@ size_t linear_bf16_workspace_bytes(bool a_tr, bool b_tr, int64_t M, int64_t N, i
   return splits > 1 ? (size_t)splits * M * N * sizeof(float) : 0;
 }
 
-int launch_linear_bf16(const Product& p, void* ws, void* stream) {
+int launch_linear_bf16(const Product& p, void* ws, LinearSums& left, void* stream) {
   const Plan plan = plan_of(p.a_tr, p.b_tr, p.M, p.N, p.K);
+  left = {};
   if (plan.shape < 0) return launch_linear_few_rows(p, stream);
-  LinearGemmArgs a = {static_cast<const uint16_t*>(p.A), static_cast<const uint16_t*>(p.B), p.M, p.N, p.K, p.lda, p.ldb, 0, 0,
-                      plan.splits, plan.slices_per_split};
+  const LinearGemmArgs a = args_of(p, plan);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (plan.splits == 1) return launch<uint16_t>(p.a_tr, p.b_tr, a, p.e, plan.shape, st);
   Epilogue sums = {};
   sums.Y = ws; sums.ldy = p.N; sums.M = p.M; sums.N = p.N;   // (N % 8 == 0)
-  const int rc = launch<float>(p.a_tr, p.b_tr, a, sums, plan.shape, st);
-  return rc ? rc : launch_linear_epilogue(1, {static_cast<float*>(ws), p.N, plan.splits}, p.e, stream);
+  left = {static_cast<float*>(ws), p.N, plan.splits};
+  return launch<float>(p.a_tr, p.b_tr, a, sums, plan.shape, st);
+}
+
+bool linear_bf16_pair(int64_t M, int64_t N, int64_t K, int64_t Np) {
+  const Plan x = plan_of(false, false, M, K, Np), w = plan_of(true, true, K, N, M);
+  return x.shape == kShapes - 1 && w.shape == kShapes - 1 && x.splits == 1 && w.splits == 1;
+}
+
+int launch_linear_bf16_pair(const Product& x, const Product& w, const ColumnSums& c, void* stream) {
+  LinearGemmArgs ax = args_of(x, plan_of(false, false, x.M, x.N, x.K)), aw = args_of(w, plan_of(true, true, w.M, w.N, w.K));
+  const unsigned grid_w = set_tiles<PairTile>(aw), grid_x = set_tiles<PairTile>(ax);
+  if (hipError_t e0 = LdsLimit<&linear_pair_kernel, PairTile::kLds>::ensure(); e0 != hipSuccess) return (int)e0;
+  hipLaunchKernelGGL(linear_pair_kernel, dim3(grid_w + grid_x + column_sum_blocks(c)), dim3(64 * PairTile::NW), PairTile::kLds,
+                     static_cast<hipStream_t>(stream), aw, w.e, ax, x.e, c, grid_w, grid_x);
+  return (int)hipGetLastError();
 }
 
 }  // namespace mhffn

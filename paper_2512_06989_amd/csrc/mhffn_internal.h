@@ -135,13 +135,18 @@ int launch_linear_backward(const Linear& p, const void* X, const void* W, const 
 // Y = residual + D(X), X [M][N]; Y may be X or the residual
 int launch_dropout(int dtype, const void* X, int64_t ldx, const Epilogue& e, void* stream);
 // Kernels of pointwise.hip behind the host code of linear.cpp
-struct LinearSums {   // Epilogue over `splits` partial products P [splits][M][ldp]
+struct LinearSums {   // `splits` partial products P [splits][M][ldp] that an epilogue goes over (splits = 0: none)
   const float* P;
   int64_t ldp;
   int splits;
 };
+struct ColumnSums {   // out[N] = the sum of partials [blocks][N] (blocks = 0: none)
+  const float* partials;
+  int64_t blocks, N;
+  void* out;
+};
 // C[m][n] = sum_k A(m,k) B(n,k) of the forms that launch_gemm_bf16 takes, and its epilogue: in the product's
-// kernel where it is not split, over its partial sums in `ws` otherwise
+// kernel where it is not split (`left` is none), to be gone over partial sums in `ws` otherwise
 struct Product {
   bool a_tr, b_tr;
   const void* A;
@@ -152,16 +157,21 @@ struct Product {
 };
 // bf16: N % 8 == 0 (e.N of the columns exist); row-form operands hold K % 32 == 0
 size_t linear_bf16_workspace_bytes(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K);
-int launch_linear_bf16(const Product& p, void* ws, void* stream);
+int launch_linear_bf16(const Product& p, void* ws, LinearSums& left, void* stream);
 // Its kernels for a few rows (gemm_bf16.hip): N % 32 == 0, K % 64 == 0
 int launch_linear_few_rows(const Product& p, void* stream);
-// fp32: any sizes, any strides.  The pair: dX [M][K] = dZ W^T and dW [K][N] = X^T dZ of a layer, in one launch where
-// that is worth it
+// fp32: any sizes, any strides
 size_t linear_f32_workspace_bytes(int64_t M, int64_t N, int64_t K);
-int launch_linear_f32(const Product& p, void* ws, void* stream);
-size_t linear_f32_pair_workspace_bytes(int64_t M, int64_t N, int64_t K);
-int launch_linear_f32_pair(const Product& dX, const Product& dW, void* ws, void* stream);
-int launch_linear_epilogue(int dtype, const LinearSums& s, const Epilogue& e, void* stream);
+int launch_linear_f32(const Product& p, void* ws, LinearSums& left, void* stream);
+// dX [M][K] = dZ W^T and dW [K][N] = X^T dZ of a layer in one launch.  Returns whether that is worth it at these
+// sizes (without launching: the bytes of both's partial sums)
+bool linear_f32_pair(int64_t M, int64_t N, int64_t K, size_t& dX_bytes, size_t& dW_bytes);
+int launch_linear_f32_pair(const Product& dX, const Product& dW, void* dX_ws, void* dW_ws, LinearSums& dX_left, LinearSums& dW_left, void* stream);
+// bf16: neither is split, and the sums are made in the same launch
+bool linear_bf16_pair(int64_t M, int64_t N, int64_t K, int64_t Np);
+int launch_linear_bf16_pair(const Product& dX, const Product& dW, const ColumnSums& c, void* stream);
+// What is left of one or two products and the sums of columns, in one launch
+int launch_linear_sums(int dtype, const LinearSums& a, const Epilogue& ea, const LinearSums& b, const Epilogue& eb, const ColumnSums& c, void* stream);
 // [rows][cols] (row stride ld) -> dense [rows_to][cols_to], zero outside; two at once (none: rows_to = 0)
 struct PackJob {
   const void* src;
@@ -183,7 +193,7 @@ struct LinearDz {
   Dropout drop;
 };
 int64_t linear_column_blocks(int64_t M, int64_t N);
-int launch_linear_dz(int dtype, const LinearDz& a, void* stream);
+int launch_linear_dz(int dtype, const LinearDz& a, ColumnSums& left, void* stream);
 
 // ---- whole module: projections around the fused path -------------------------
 // Problem::ldx / ldy are the row strides of the module's input X (dX) and output O (dO);

@@ -6,7 +6,7 @@
 namespace mhffn {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kSumThreads;
 
 // A thread's pieces of a [rows][cols] array, in row order: piece -> (row, first column)
 struct Pieces {
@@ -29,21 +29,34 @@ unsigned piece_blocks(int64_t pieces) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(kThreads) void linear_epilogue_kernel(LinearSums s, Epilogue e, Pieces p) {
-  const DropKey key = drop_key(e.drop);
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < p.total; i += (int64_t)gridDim.x * kThreads) {
-    int64_t row, col;
-    piece_at(p, i, row, col);
-    const int cols = (int)(s.ldp - col < 8 ? s.ldp - col : 8);
-    float v[8];
-    load8(s.P + row * s.ldp + col, cols, v);
-    for (int k = 1; k < s.splits; ++k) {
-      float w[8];
-      load8(s.P + ((int64_t)k * e.M + row) * s.ldp + col, cols, w);
+__device__ __forceinline__ void linear_sum(const LinearSums& s, const Epilogue& e, const Pieces& p, int64_t i, const DropKey& key) {
+  int64_t row, col;
+  piece_at(p, i, row, col);
+  const int cols = (int)(s.ldp - col < 8 ? s.ldp - col : 8);
+  float v[8];
+  load8(s.P + row * s.ldp + col, cols, v);
+  for (int k = 1; k < s.splits; ++k) {
+    float w[8];
+    load8(s.P + ((int64_t)k * e.M + row) * s.ldp + col, cols, w);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += w[j];
-    }
-    epilogue8<T>(v, row, col, e, key);
+    for (int j = 0; j < 8; ++j) v[j] += w[j];
+  }
+  epilogue8<T>(v, row, col, e, key);
+}
+// What one or two products left (pieces of the first, then of the second), and in the first `blocks_c` workgroups sums of columns
+template <typename T>
+__global__ __launch_bounds__(kSumThreads) void linear_sums_kernel(LinearSums a, Epilogue ea, Pieces pa, LinearSums b, Epilogue eb, Pieces pb,
+                                                                  ColumnSums c, unsigned blocks_c) {
+  __shared__ float sums[kSumThreads];
+  if (blockIdx.x < blocks_c) {
+    column_sums<T>(c, blockIdx.x, sums);
+    return;
+  }
+  const DropKey key = drop_key(ea.drop);   // (the second is a gradient: no dropout)
+  for (int64_t i = (int64_t)(blockIdx.x - blocks_c) * kThreads + threadIdx.x; i < pa.total + pb.total;
+       i += (int64_t)(gridDim.x - blocks_c) * kThreads) {
+    if (i < pa.total) linear_sum<T>(a, ea, pa, i, key);
+    else linear_sum<T>(b, eb, pb, i - pa.total, DropKey{});
   }
 }
 
@@ -122,26 +135,6 @@ __global__ __launch_bounds__(kThreads) void linear_dz_kernel(LinearDz a, DzGrid 
   }
 }
 
-// 32 columns a workgroup: thread (column t % 32, t / 32) adds up every eighth row block, the eight sums meet
-// in LDS (one thread a column waited for each of its loads: 128 row blocks of 1024 columns took 31 us)
-template <typename T>
-__global__ __launch_bounds__(kThreads) void column_sum_kernel(const float* partials, int64_t blocks, int64_t N, T* out) {
-  __shared__ float sums[kThreads];
-  const int64_t c = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
-  float sum = 0.f;
-  if (c < N) {
-#pragma unroll 8
-    for (int64_t b = threadIdx.x >> 5; b < blocks; b += 8) sum += partials[b * N + c];
-  }
-  sums[threadIdx.x] = sum;
-  __syncthreads();
-  if (threadIdx.x >= 32 || c >= N) return;
-#pragma unroll
-  for (int k = 1; k < 8; ++k) sum += sums[32 * k + threadIdx.x];
-  if constexpr (sizeof(T) == 2) out[c] = (uint16_t)pack_bf16(sum, 0.f);
-  else out[c] = sum;
-}
-
 DzGrid dz_grid(int64_t M, int64_t N, int64_t cols_to) {
   DzGrid g;
   g.pieces = ((cols_to > N ? cols_to : N) + 7) / 8;
@@ -160,12 +153,16 @@ int64_t linear_column_blocks(int64_t M, int64_t N) {
   return most < want ? (most > 0 ? most : 1) : want;
 }
 
-int launch_linear_epilogue(int dtype, const LinearSums& s, const Epilogue& e, void* stream) {
-  const Pieces p = make_pieces(e.M, e.N);
-  if (p.total == 0) return 0;
+int launch_linear_sums(int dtype, const LinearSums& a, const Epilogue& ea, const LinearSums& b, const Epilogue& eb,
+                       const ColumnSums& c, void* stream) {
+  const Pieces pa = a.splits ? make_pieces(ea.M, ea.N) : make_pieces(0, 0), pb = b.splits ? make_pieces(eb.M, eb.N) : make_pieces(0, 0);
+  const unsigned blocks_c = column_sum_blocks(c), blocks = piece_blocks(pa.total + pb.total);
+  if (blocks_c + blocks == 0) return 0;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dtype == 1) hipLaunchKernelGGL(linear_epilogue_kernel<uint16_t>, dim3(piece_blocks(p.total)), dim3(kThreads), 0, st, s, e, p);
-  else hipLaunchKernelGGL(linear_epilogue_kernel<float>, dim3(piece_blocks(p.total)), dim3(kThreads), 0, st, s, e, p);
+  if (dtype == 1)
+    hipLaunchKernelGGL(linear_sums_kernel<uint16_t>, dim3(blocks_c + blocks), dim3(kSumThreads), 0, st, a, ea, pa, b, eb, pb, c, blocks_c);
+  else
+    hipLaunchKernelGGL(linear_sums_kernel<float>, dim3(blocks_c + blocks), dim3(kSumThreads), 0, st, a, ea, pa, b, eb, pb, c, blocks_c);
   return (int)hipGetLastError();
 }
 
@@ -192,23 +189,16 @@ int launch_pack(int dtype, const PackJob& a, const PackJob& b, void* stream) {
   return (int)hipGetLastError();
 }
 
-int launch_linear_dz(int dtype, const LinearDz& a, void* stream) {
+int launch_linear_dz(int dtype, const LinearDz& a, ColumnSums& left, void* stream) {
+  left = {};
   if (!a.dZ && !a.dbias) return 0;
   const DzGrid g = dz_grid(a.M, a.N, a.dZ ? a.ldz : a.N);
   const int64_t blocks = linear_column_blocks(a.M, a.N);
   const dim3 grid((unsigned)((g.pieces + (1 << g.lane_shift) - 1) >> g.lane_shift), (unsigned)blocks);
-  const dim3 sum_grid((unsigned)((a.N + 31) / 32));
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dtype == 1) hipLaunchKernelGGL(linear_dz_kernel<uint16_t>, grid, dim3(kThreads), 0, st, a, g);
   else hipLaunchKernelGGL(linear_dz_kernel<float>, grid, dim3(kThreads), 0, st, a, g);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.dbias) return (int)e;
-  if (dtype == 1)
-    hipLaunchKernelGGL(column_sum_kernel<uint16_t>, sum_grid, dim3(kThreads), 0, st, a.partials, blocks, a.N,
-                       static_cast<uint16_t*>(a.dbias));
-  else
-    hipLaunchKernelGGL(column_sum_kernel<float>, sum_grid, dim3(kThreads), 0, st, a.partials, blocks, a.N,
-                       static_cast<float*>(a.dbias));
+  if (a.dbias) left = {a.partials, blocks, a.N, a.dbias};
   return (int)hipGetLastError();
 }
 
