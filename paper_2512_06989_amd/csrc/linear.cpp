@@ -138,7 +138,8 @@ std::string linear_plan(const Linear& p, bool back) {
   if (p.dtype != 1) return s + (back ? linear_f32_pair_plan(p.M, p.N, p.K) : linear_f32_plan(p.M, p.N, p.K));
   const int64_t K8 = up(p.K, 8), N8 = up(p.N, 8);
   if (!back) return s + linear_bf16_plan(false, true, p.M, forward_columns(p, o), o.x || o.w ? o.Kp : p.K);
-  return s + "dX " + linear_bf16_plan(false, false, p.M, K8, o.Np) + (linear_bf16_pair(p.M, N8, K8, o.Np) ? " with dW " : "; dW ") + linear_bf16_plan(true, true, K8, N8, p.M);
+  if (linear_bf16_pair(p.M, N8, K8, o.Np)) return s + linear_bf16_pair_plan();
+  return s + "dX " + linear_bf16_plan(false, false, p.M, K8, o.Np) + "; dW " + linear_bf16_plan(true, true, K8, N8, p.M);
 }
 
 size_t linear_workspace_bytes(const Linear& p, bool back) {

@@ -317,26 +317,28 @@ __global__ __launch_bounds__(512, 2) void linear_gemm_kernel(LinearGemmArgs a, E
 }
 
 // ---------------------------------------------------------------------------
-// Smaller tiles, for outputs that would leave CUs without one: two rows of waves, k in units of 64.  Such products wait for memory, so what counts is bytes in flight: units lie in a ring that
-// fills LDS (five of 32 KB .. ten of 16 KB), all but one of them under way.  A wave multiplies a unit's operands from
-// registers and between the products reads the next one's from LDS and requests another, an instruction at a
-// time; one wait for LDS and one barrier per unit (two steps of 32 with a wait each: 730 clocks a unit of 64 x 64).
-// Images and operands as above, a transposed unit [64 k][64] per 64 columns.
+// Smaller tiles, for outputs that would leave CUs without one: two rows of waves, k in units of 64.  Such products wait
+// for memory, so what counts is bytes in flight: units lie in a ring of 48 KB (64 x 64) .. 160 KB (128 x 128), all but
+// one of them under way, and up to three workgroups share a CU, so that one's first loads and epilogue lie under
+// another's products (1000 x 1024 x 2816: 14.9 us; 64 x 64 with all of LDS to itself 24.4, 128 x 128 16.0).  A wave
+// multiplies a unit's operands from registers and between the products reads the next one's from LDS and requests
+// another, an instruction at a time; one wait for LDS and one barrier per unit (two steps of 32 with a wait each:
+// 730 clocks a unit of 64 x 64).  Images and operands as above, a transposed unit [64 k][64] per 64 columns.
 // ---------------------------------------------------------------------------
-template <int BM_, int BN_, int WN_, int NK_>
+template <int BM_, int BN_, int WN_, int PER_CU>
 struct SmallTile {
   static constexpr int BM = BM_, BN = BN_, WN = WN_, NW = 2 * WN, TM = BM / 2, TN = BN / WN, IM = TM / 16, IN = TN / 16;
-  static constexpr int NK = NK_, kK = 64 * NK;             // k of a unit: NK images [..][64 k] of each side
-  static constexpr int kSubA = BM * 128, kSubB = BN * 128, kUnitA = NK * kSubA, kUnit = NK * (kSubA + kSubB);
-  static constexpr int kSlots = (int)kLdsBytesPerWorkgroup / kUnit, kLds = kSlots * kUnit;
-  static constexpr int kLoadsA = kUnitA / 1024 / NW, kLoadsB = NK * kSubB / 1024 / NW, kLoads = kLoadsA + kLoadsB;   // 1 KB loads per unit of each wave
-  static_assert(BM % 64 == 0 && BN % 64 == 0 && TN % 32 == 0 && kLds >= NW * 32 * TN * 4 && kLoads * (kSlots - 1) < 64, "");
+  static constexpr int kK = 64;                            // k of a unit
+  static constexpr int kUnitA = BM * 128, kUnitB = BN * 128, kUnit = kUnitA + kUnitB;
+  static constexpr int kPerCu = PER_CU, kSlots = (int)kLdsBytesPerWorkgroup / PER_CU / kUnit, kLds = kSlots * kUnit;
+  static constexpr int kLoadsA = kUnitA / 1024 / NW, kLoadsB = kUnitB / 1024 / NW, kLoads = kLoadsA + kLoadsB;   // 1 KB loads per unit of each wave
+  static_assert(BM % 64 == 0 && BN % 64 == 0 && TN % 32 == 0 && kSlots > 1 && kLds >= NW * 32 * TN * 4 && kLoads * (kSlots - 1) < 64, "");
   static_assert(kLoadsA * NW * 1024 == kUnitA && kLoads * NW * 1024 == kUnit, "whole loads");
 };
 
 template <bool A_TR, bool B_TR, typename G, typename T>
 __device__ __forceinline__ void linear_small_tile(const LinearGemmArgs& a, Epilogue e, int64_t block, unsigned char* smem) {
-  constexpr int IM = G::IM, IN = G::IN, OPS = IM + IN, NM = IM * IN, S = G::kSlots, NS = 2 * G::NK;   // operands and products of 32 k, of which a unit has NS
+  constexpr int IM = G::IM, IN = G::IN, OPS = IM + IN, NM = IM * IN, S = G::kSlots, NS = 2;   // operands and products of 32 k, of which a unit has NS
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i16 = lane & 15, gq = lane >> 4;
   const int wm = wave / G::WN, wn = wave % G::WN;
@@ -347,30 +349,28 @@ __device__ __forceinline__ void linear_small_tile(const LinearGemmArgs& a, Epilo
   const int units = (int)((kend - kbase + NS - 1) / NS);
 
   // ---- requests: of a side's 1 KB images wave w moves NW q + w -------------------------------------
-  // k past the product's end: row form fetches the unit's first 64, or the first 32 of 64, again, k rows repeat the last.
+  // k past the product's end: row form fetches the first 32 of 64 again, k rows repeat the last.
   unsigned ga[G::kLoadsA], gb[G::kLoadsB];
-  auto place = [&](bool tr, int q, int64_t ld, int64_t row0, int64_t rows, int images, int64_t left) __attribute__((always_inline)) -> unsigned {
-    const int img = G::NW * q + wave, sub = img / images, i = img % images;   // images: 1 KB images of 64 k of this side
-    int64_t most_k = left - 64 * sub;                                          // k of them that exist
+  auto place = [&](bool tr, int q, int64_t ld, int64_t row0, int64_t rows, int64_t left) __attribute__((always_inline)) -> unsigned {
+    const int i = G::NW * q + wave;
     if (!tr) {
-      const int row = 8 * i + (lane >> 3), k = most_k > 0 ? 64 * sub : 0;
+      const int row = 8 * i + (lane >> 3);
       int chunk = (lane & 7) ^ ((row >> 1) & 7);
-      if (most_k <= kStep) chunk &= 3;
+      if (left <= kStep) chunk &= 3;
       const int64_t gr = row0 + row < rows ? row : rows - 1 - row0;
-      return (unsigned)((gr * ld + k) * 2 + (chunk << 4));
+      return (unsigned)(gr * ld * 2 + (chunk << 4));
     }
     int64_t kr = 8 * (i & 7) + (lane >> 3);
     int64_t gc = row0 + 64 * (i >> 3) + (((lane & 7) ^ tr_flip((int)kr)) << 3);
     gc = (gc + 8 <= rows ? gc : rows - 8) - row0;
-    kr += 64 * sub;
     kr = kr < left ? kr : left - 1;
     return (unsigned)((kr * ld + gc) * 2);
   };
   auto offsets = [&](int64_t left) __attribute__((always_inline)) {
 #pragma unroll
-    for (int q = 0; q < G::kLoadsA; ++q) ga[q] = place(A_TR, q, a.lda, m0, a.M, G::kSubA / 1024, left);
+    for (int q = 0; q < G::kLoadsA; ++q) ga[q] = place(A_TR, q, a.lda, m0, a.M, left);
 #pragma unroll
-    for (int q = 0; q < G::kLoadsB; ++q) gb[q] = place(B_TR, q, a.ldb, n0, a.N, G::kSubB / 1024, left);
+    for (int q = 0; q < G::kLoadsB; ++q) gb[q] = place(B_TR, q, a.ldb, n0, a.N, left);
   };
   const unsigned char* pa = uniform(reinterpret_cast<const unsigned char*>(a.A + (A_TR ? m0 + k0 * a.lda : m0 * a.lda + k0)));
   const unsigned char* pb = uniform(reinterpret_cast<const unsigned char*>(a.B + (B_TR ? n0 + k0 * a.ldb : n0 * a.ldb + k0)));
@@ -432,14 +432,13 @@ __device__ __forceinline__ void linear_small_tile(const LinearGemmArgs& a, Epilo
   };
   Operands f0, f1;
   auto read = [&](auto C_, Operands& f) __attribute__((always_inline)) {
-    constexpr int c = decltype(C_)::value, sub = c / OPS / 2, HALF = c / OPS % 2, o = c % OPS, idx = o < IN ? o : o - IN;
-    constexpr int off = sub * (o < IN ? G::kSubB : G::kSubA);
+    constexpr int c = decltype(C_)::value, HALF = c / OPS, o = c % OPS, idx = o < IN ? o : o - IN;
     if constexpr (o < IN ? B_TR : A_TR) {
       const unsigned at = o < IN ? at_b[B_TR ? idx : 0] : at_a[A_TR ? idx : 0];
-      f.lo[c] = lds_read_tr16_untracked<off + HALF * 4096>(at);
-      f.hi[c] = lds_read_tr16_untracked<off + HALF * 4096 + 512>(at);
+      f.lo[c] = lds_read_tr16_untracked<HALF * 4096>(at);
+      f.hi[c] = lds_read_tr16_untracked<HALF * 4096 + 512>(at);
     } else {
-      f.full[c] = lds_read_b128_untracked<off + 2048 * idx>(o < IN ? at_b[HALF] : at_a[HALF]);
+      f.full[c] = lds_read_b128_untracked<2048 * idx>(o < IN ? at_b[HALF] : at_a[HALF]);
     }
   };
   auto arrived = [&](Operands& f, int unit) __attribute__((always_inline)) {
@@ -546,13 +545,13 @@ __device__ __forceinline__ void linear_small_tile(const LinearGemmArgs& a, Epilo
 }
 
 template <bool A_TR, bool B_TR, typename G, typename T>
-__global__ __launch_bounds__(64 * G::NW, G::NW / 4) void linear_small_kernel(LinearGemmArgs a, Epilogue e) {
+__global__ __launch_bounds__(64 * G::NW, G::kPerCu * G::NW / 4) void linear_small_kernel(LinearGemmArgs a, Epilogue e) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   linear_small_tile<A_TR, B_TR, G, T>(a, e, blockIdx.x, smem);
 }
 // A backward of few tiles: dW, dX and dbias in one launch
-using PairTile = SmallTile<64, 64, 2, 2>;
-__global__ __launch_bounds__(64 * PairTile::NW, PairTile::NW / 4) void linear_pair_kernel(LinearGemmArgs w, Epilogue ew, LinearGemmArgs x, Epilogue ex,
+using PairTile = SmallTile<64, 64, 2, 3>;
+__global__ __launch_bounds__(64 * PairTile::NW, PairTile::kPerCu * PairTile::NW / 4) void linear_pair_kernel(LinearGemmArgs w, Epilogue ew, LinearGemmArgs x, Epilogue ex,
                                                                                      ColumnSums c, unsigned grid_w, unsigned grid_x) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   static_assert(64 * PairTile::NW == kSumThreads, "");
@@ -585,7 +584,7 @@ int launch_form(const LinearGemmArgs& a, const Epilogue& e, int shape, hipStream
     case 0: return launch_tile<false, A_TR, B_TR, Tile<A_TR, B_TR, 256, 256, 2, 4>, T>(a, e, stream);
     case 1: return launch_tile<false, A_TR, B_TR, Tile<A_TR, B_TR, 256, 128, 4, 2>, T>(a, e, stream);
     case 2: return launch_tile<true, A_TR, B_TR, SmallTile<128, 128, 4, 1>, T>(a, e, stream);
-    case 3: return launch_tile<true, A_TR, B_TR, SmallTile<64, 128, 2, 1>, T>(a, e, stream);
+    case 3: return launch_tile<true, A_TR, B_TR, SmallTile<64, 128, 2, 2>, T>(a, e, stream);
     default: return launch_tile<true, A_TR, B_TR, PairTile, T>(a, e, stream);
   }
 }
@@ -596,33 +595,38 @@ int launch(bool a_tr, bool b_tr, const LinearGemmArgs& a, const Epilogue& e, int
   return a_tr && b_tr ? launch_form<true, true, T>(a, e, shape, stream) : -1;   // transposed A with row-form B: no caller
 }
 
-// Tile shape and split of the contraction, by the time of the fullest CU.  Microseconds measured: a slice of k costs a
-// workgroup kSliceUs, what lies around its slices kAroundUs; the sum over the splits is a launch of 6 and moves
-// 5.7 MB a us.  The kernels for few rows: up to 16 (weights in row form: 8) 16 columns a workgroup, above 32 x 32.
-struct Plan { int shape, splits; int64_t slices_per_split; };   // shape -1: the kernels for few rows
+// Tile shape and split of the contraction.  Microseconds measured, with n tiles on the fullest CU: a slice of k takes
+// kSliceUs[0] + n kSliceUs[1] (what is shared by the workgroups of a CU hides a latency), what lies around the slices
+// kAroundUs[0] + n kAroundUs[1]; the sum over the splits is a launch of 4 and moves 5.7 MB a us.  The kernels for
+// few rows: up to 16 (weights in row form: 8) 16 columns a workgroup, above 32 x 32.
+struct Plan { int shape, splits; int64_t slices_per_split; double cost; };   // shape -1: the kernels for few rows
 constexpr int kShapes = 5, kShapeM[kShapes] = {256, 256, 128, 64, 64}, kShapeN[kShapes] = {256, 128, 128, 128, 64};
-constexpr double kSliceUs[kShapes] = {0.74, 0.5, 0.3, 0.21, 0.125}, kAroundUs[kShapes] = {12, 5, 2.5, 1, 1};
+constexpr double kSliceUs[kShapes][2] = {{0, 0.72}, {0, 0.48}, {0, 0.277}, {0.045, 0.128}, {0.04, 0.08}};
+constexpr double kAroundUs[kShapes][2] = {{1, 12}, {3, 6}, {2, 4}, {3.5, 1.6}, {3.3, 0.73}};
+int64_t tiles_of(int sh, int64_t M, int64_t N) { return ((M + kShapeM[sh] - 1) / kShapeM[sh]) * ((N + kShapeN[sh] - 1) / kShapeN[sh]); }
 Plan plan_of(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K) {
   const int64_t KT = (K + kStep - 1) / kStep;
-  Plan best{0, 1, KT};
-  double least = 0.0;
+  Plan best{0, 1, KT, 0.0};
   for (int sh = 0; sh < kShapes; ++sh) {
-    const int64_t tiles = ((M + kShapeM[sh] - 1) / kShapeM[sh]) * ((N + kShapeN[sh] - 1) / kShapeN[sh]);
+    const int64_t tiles = tiles_of(sh, M, N);
     for (int want = 1; want <= 16; ++want) {
       const int64_t per = (KT + want - 1) / want;
       if (want > 1 && (per < 8 || (KT + per - 1) / per != want)) continue;   // at least eight slices per workgroup
-      double cost = (double)((tiles * want + 255) / 256) * (per * kSliceUs[sh] + kAroundUs[sh]);
-      if (want > 1) cost += 6 + (double)want * M * N * 4 / 5.7e6;
-      if (least == 0.0 || cost < least) { least = cost; best = {sh, want, per}; }
+      const double n = (double)((tiles * want + 255) / 256);
+      double cost = (double)per * (kSliceUs[sh][0] + kSliceUs[sh][1] * n) + kAroundUs[sh][0] + kAroundUs[sh][1] * n;
+      if (want > 1) cost += 4 + (double)want * M * N * 4 / 5.7e6;
+      if (best.cost == 0.0 || cost < best.cost) best = {sh, want, per, cost};
     }
   }
   if (!a_tr && N % 32 == 0 && K % 64 == 0) {
     const bool few = M <= (b_tr ? 16 : 8);
     const int64_t wgs = few ? N / 16 : (M + 31) / 32 * (N / 32);
-    if ((double)((wgs + 255) / 256) * (K / 64 * (few ? 0.12 : 0.2) + 0.7) < least) best = {-1, 1, KT};
+    const double cost = 3 + (double)((wgs + 255) / 256) * (K / 64 * (few ? 0.12 : 0.2) + 0.7);
+    if (cost < best.cost) best = {-1, 1, KT, cost};
   }
   return best;
 }
+Plan pair_plan(int64_t K) { return {kShapes - 1, 1, (K + kStep - 1) / kStep, 0.0}; }
 LinearGemmArgs args_of(const Product& p, const Plan& plan) {
   return {static_cast<const uint16_t*>(p.A), static_cast<const uint16_t*>(p.B), p.M, p.N, p.K, p.lda, p.ldb, 0, 0, plan.splits,
           plan.slices_per_split};
@@ -635,6 +639,8 @@ std::string linear_bf16_plan(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t
   if (p.shape < 0) return "few rows";
   return std::to_string(kShapeM[p.shape]) + "x" + std::to_string(kShapeN[p.shape]) + " splits=" + std::to_string(p.splits);
 }
+
+std::string linear_bf16_pair_plan() { return "dX 64x64 splits=1 with dW 64x64 splits=1"; }
 
 size_t linear_bf16_workspace_bytes(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K) {
   const int splits = plan_of(a_tr, b_tr, M, N, K).splits;
@@ -654,13 +660,18 @@ int launch_linear_bf16(const Product& p, void* ws, LinearSums& left, void* strea
   return launch<float>(p.a_tr, p.b_tr, a, sums, plan.shape, st);
 }
 
+// By the longer product and the mean of a CU's slices
 bool linear_bf16_pair(int64_t M, int64_t N, int64_t K, int64_t Np) {
-  const Plan x = plan_of(false, false, M, K, Np), w = plan_of(true, true, K, N, M);
-  return x.shape == kShapes - 1 && w.shape == kShapes - 1 && x.splits == 1 && w.splits == 1;
+  constexpr int kTile = kShapes - 1;
+  const double kx = (double)pair_plan(Np).slices_per_split, kw = (double)pair_plan(M).slices_per_split, longest = kx > kw ? kx : kw;
+  const double tx = (double)tiles_of(kTile, M, K), tw = (double)tiles_of(kTile, K, N);
+  const double cost = longest * kSliceUs[kTile][0] + (longest / 2 + (tx * kx + tw * kw) / 256) * kSliceUs[kTile][1] + kAroundUs[kTile][0] +
+                      kAroundUs[kTile][1] * (tx + tw) / 256;
+  return cost < plan_of(false, false, M, K, Np).cost + plan_of(true, true, K, N, M).cost;
 }
 
 int launch_linear_bf16_pair(const Product& x, const Product& w, const ColumnSums& c, void* stream) {
-  LinearGemmArgs ax = args_of(x, plan_of(false, false, x.M, x.N, x.K)), aw = args_of(w, plan_of(true, true, w.M, w.N, w.K));
+  LinearGemmArgs ax = args_of(x, pair_plan(x.K)), aw = args_of(w, pair_plan(w.K));
   const unsigned grid_w = set_tiles<PairTile>(aw), grid_x = set_tiles<PairTile>(ax);
   if (hipError_t e0 = LdsLimit<&linear_pair_kernel, PairTile::kLds>::ensure(); e0 != hipSuccess) return (int)e0;
   hipLaunchKernelGGL(linear_pair_kernel, dim3(grid_w + grid_x + column_sum_blocks(c)), dim3(64 * PairTile::NW), PairTile::kLds,

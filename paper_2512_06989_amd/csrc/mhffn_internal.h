@@ -233,6 +233,7 @@ int gemm_bf16_few_columns(bool b_tr, int64_t M, int64_t N, int64_t K);
 std::string module_plan(const Problem& p, int dtype, bool backward);
 std::string linear_plan(const Linear& p, bool backward);
 std::string linear_bf16_plan(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K);
+std::string linear_bf16_pair_plan();
 std::string linear_f32_plan(int64_t M, int64_t N, int64_t K);
 std::string linear_f32_pair_plan(int64_t M, int64_t N, int64_t K);
 
