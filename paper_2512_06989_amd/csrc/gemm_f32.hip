@@ -317,9 +317,9 @@ int launch_linear_f32_pair(const Product& x, const Product& w, void* ws_x, void*
   constexpr int kLdsW = lds_of<true, true, kPairTile>(), kLdsX = lds_of<false, false, kPairTile>(), kLds = kLdsW > kLdsX ? kLdsW : kLdsX;
   const F32Pair plan = plan_f32_pair(x.M, x.K, x.N);
   const GemmF32Args aw = args_of(w, plan.w), ax = args_of(x, plan.x);
-  const unsigned grid_w = (unsigned)xcd_grid_size(aw.n_items), grid_x = (unsigned)xcd_grid_size(ax.n_items);
-  left_x = left_of(x, plan.x, ws_x);
-  left_w = left_of(w, plan.w, ws_w);
+  const unsigned grid_w = w.e.Y ? (unsigned)xcd_grid_size(aw.n_items) : 0, grid_x = x.e.Y ? (unsigned)xcd_grid_size(ax.n_items) : 0;
+  left_x = x.e.Y ? left_of(x, plan.x, ws_x) : LinearSums{};
+  left_w = w.e.Y ? left_of(w, plan.w, ws_w) : LinearSums{};
   if (hipError_t e0 = LdsLimit<&gemm_f32_pair_kernel, kLds>::ensure(); e0 != hipSuccess) return (int)e0;
   hipLaunchKernelGGL(gemm_f32_pair_kernel, dim3(grid_w + grid_x), dim3(kFThreads), kLds, static_cast<hipStream_t>(stream), aw,
                      epilogue_of(w, plan.w, ws_w), ax, epilogue_of(x, plan.x, ws_x), grid_w);

@@ -96,12 +96,14 @@ int backward(const Linear& p, const void* X, const void* W, const void* Z, const
   void* const dZ = o.dz ? arena.take((size_t)p.M * ldz * elt(p.dtype)) : nullptr;
   float* const sums = static_cast<float*>(arena.take((size_t)linear_column_blocks(p.M, p.N) * p.N * 4));
   // Both products at once, or one after the other; what is split is added up at the end
-  size_t px, pw;
+  size_t px = 0, pw = 0;
   const bool pair = bf16 ? linear_bf16_pair(p.M, N8, K8, o.Np) : linear_f32_pair(p.M, p.N, p.K, px, pw);
-  const size_t ax = partial_bytes(p.dtype, false, false, p.M, K8, o.Np), aw = partial_bytes(p.dtype, true, true, K8, N8, p.M);
-  if (bf16 || !pair) px = pw = 0;
-  void* const Px = arena.take(ax > px ? ax : px);
-  void* const Pw = arena.take(aw > pw ? aw : pw);
+  if (!pair) {
+    px = partial_bytes(p.dtype, false, false, p.M, K8, o.Np);
+    pw = partial_bytes(p.dtype, true, true, K8, N8, p.M);
+  }
+  void* const Px = arena.take(px);
+  void* const Pw = arena.take(pw);
   if (bytes) {
     *bytes = arena.used;
     return 0;
@@ -117,7 +119,7 @@ int backward(const Linear& p, const void* X, const void* W, const void* Z, const
   const Product x = {false, false, G, ldg, o.w ? Wp : W, o.w ? o.Np : p.N, p.M, K8, o.Np, plain(dX, p.ldx, p.M, p.K)};
   const Product w = {true, true, o.x ? Xp : X, o.x ? o.Kp : p.ldx, G, ldg, K8, N8, p.M, plain(dW, p.N, p.K, p.N)};
   LinearSums left_x = {}, left_w = {};
-  if (dX && dW && pair) {
+  if (pair && (dX || dW)) {   // (one alone too: its bits do not depend on what else is asked for)
     if (bf16) return launch_linear_bf16_pair(x, w, columns, stream);
     rc = launch_linear_f32_pair(x, w, Px, Pw, left_x, left_w, stream);
   } else {

@@ -672,7 +672,7 @@ bool linear_bf16_pair(int64_t M, int64_t N, int64_t K, int64_t Np) {
 
 int launch_linear_bf16_pair(const Product& x, const Product& w, const ColumnSums& c, void* stream) {
   LinearGemmArgs ax = args_of(x, pair_plan(x.K)), aw = args_of(w, pair_plan(w.K));
-  const unsigned grid_w = set_tiles<PairTile>(aw), grid_x = set_tiles<PairTile>(ax);
+  const unsigned grid_w = w.e.Y ? set_tiles<PairTile>(aw) : 0, grid_x = x.e.Y ? set_tiles<PairTile>(ax) : 0;
   if (hipError_t e0 = LdsLimit<&linear_pair_kernel, PairTile::kLds>::ensure(); e0 != hipSuccess) return (int)e0;
   hipLaunchKernelGGL(linear_pair_kernel, dim3(grid_w + grid_x + column_sum_blocks(c)), dim3(64 * PairTile::NW), PairTile::kLds,
                      static_cast<hipStream_t>(stream), aw, w.e, ax, x.e, c, grid_w, grid_x);

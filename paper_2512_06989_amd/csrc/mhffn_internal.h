@@ -164,7 +164,7 @@ int launch_linear_few_rows(const Product& p, void* stream);
 size_t linear_f32_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int launch_linear_f32(const Product& p, void* ws, LinearSums& left, void* stream);
 // dX [M][K] = dZ W^T and dW [K][N] = X^T dZ of a layer in one launch.  Returns whether that is worth it at these
-// sizes (without launching: the bytes of both's partial sums)
+// sizes (without launching: the bytes of both's partial sums).  e.Y = NULL: that one is not wanted
 bool linear_f32_pair(int64_t M, int64_t N, int64_t K, size_t& dX_bytes, size_t& dW_bytes);
 int launch_linear_f32_pair(const Product& dX, const Product& dW, void* dX_ws, void* dW_ws, LinearSums& dX_left, LinearSums& dW_left, void* stream);
 // bf16: neither is split, and the sums are made in the same launch
