@@ -271,9 +271,9 @@ int mhffn_module_backward(const mhffn_desc* desc, const void* X, const void* W_i
  * what its forward was given.  `call` tells the dropouts of one step apart.  With T = 0 rng
  * may be NULL.
  *
- * n_rows, d_in and d_out take any size (rows from 0, widths from 1 to 2^20), row strides any
- * that is at least the width; rows that are not 16-byte aligned, and widths that are no
- * multiple of 32, cost copies of the operands in the workspace.  Arithmetic is fp32 (bf16:
+ * n_rows, d_in and d_out take any size (rows from 0 to 2^28, widths from 1 to 2^20), row strides any
+ * that is at least the width; rows that are not 16-byte aligned or lie more than 2^22 elements apart, and
+ * widths that are no multiple of 32, cost copies of the operands in the workspace (fp32: only the rows far apart).  Arithmetic is fp32 (bf16:
  * products on the bf16 MFMA); Z and Y are rounded once to the storage type, and the
  * activation sees the unrounded Z.  The backward of an activation uses the rounded Z it is
  * given, and dZ is rounded to the storage type once more as an operand of its two products
@@ -310,7 +310,7 @@ int mhffn_linear_forward(const mhffn_linear_desc* desc, const void* X, const voi
 
 /* dZ = D(dY) act'(Z);  dX = dZ W^T;  dW = X^T dZ;  dbias = the column sums of dZ.  Any
  * gradient may be NULL => not computed.  Z is read unless the activation is none (relu'(0) = 0).  The
- * gradient of the residual is dY itself. */
+ * gradient of the residual is dY itself.  No gradient may overlap an input. */
 int mhffn_linear_backward(const mhffn_linear_desc* desc, const void* X, const void* W,
                           const void* Z, const void* dY, const void* rng, void* dX, void* dW,
                           void* dbias, void* workspace, size_t workspace_bytes,

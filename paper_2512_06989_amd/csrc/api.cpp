@@ -103,11 +103,12 @@ int check_dropout(float p, const void* rng, uint64_t call, bool reads, mhffn::Dr
   return (reinterpret_cast<uintptr_t>(rng) & 7u) ? MHFFN_ERR_ALIGN : MHFFN_OK;
 }
 
-constexpr int64_t kMostRows = (int64_t)1 << 40, kMostWidth = 1 << 20;
+// (linear: a launch holds fewer than 2^32 threads, and the narrowest tiles take four a row)
+constexpr int64_t kMostRows = (int64_t)1 << 40, kMostLinearRows = 1 << 28, kMostWidth = 1 << 20;
 
 int check_linear(const mhffn_linear_desc* d, const void* rng, mhffn::Linear* p) {
   if (!d) return MHFFN_ERR_NULL;
-  if (d->n_rows < 0 || d->n_rows > kMostRows || d->d_in < 1 || d->d_out < 1 || d->d_in > kMostWidth ||
+  if (d->n_rows < 0 || d->n_rows > kMostLinearRows || d->d_in < 1 || d->d_out < 1 || d->d_in > kMostWidth ||
       d->d_out > kMostWidth)
     return MHFFN_ERR_SHAPE;
   if (d->dtype != MHFFN_F32 && d->dtype != MHFFN_BF16) return MHFFN_ERR_UNSUPPORTED;

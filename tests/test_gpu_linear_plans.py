@@ -36,6 +36,14 @@ def test_the_sizes_take_different_ways():
     assert "" not in ways and len(ways) > 20
 
 
+def test_rows_that_no_launch_could_count():
+    lib = mhffn.load()
+    for rows, works in ((2 ** 28, True), (2 ** 28 + 1, False), (2 ** 40, False)):
+        d = mhffn.LinearDesc(rows, 33, 8, 0, 0, 0, 1, 0, 0.0, 0)
+        for op in (8, 9):
+            assert (lib.mhffn_linear_workspace_bytes(ctypes.byref(d), op) > 0) == works
+
+
 def some(n, most=96):
     """Up to `most` indices below n: both ends, the edges of tiles, an odd step between."""
     edges = {i for e in (64, 128, 256, n) for i in (e - 1, e, n // e * e, n // e * e - 1)} | {0, n - 1}
