@@ -549,15 +549,17 @@ __global__ __launch_bounds__(64 * G::NW, G::kPerCu * G::NW / 4) void linear_smal
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   linear_small_tile<A_TR, B_TR, G, T>(a, e, blockIdx.x, smem);
 }
-// A backward of few tiles: dW, dX and dbias in one launch
+// A backward of few tiles: dX, dW and the sums of columns in one launch.  Workgroups start in order: the longer
+// product's come first.
 using PairTile = SmallTile<64, 64, 2, 3>;
-__global__ __launch_bounds__(64 * PairTile::NW, PairTile::kPerCu * PairTile::NW / 4) void linear_pair_kernel(LinearGemmArgs w, Epilogue ew, LinearGemmArgs x, Epilogue ex,
-                                                                                     ColumnSums c, unsigned grid_w, unsigned grid_x) {
+__global__ __launch_bounds__(64 * PairTile::NW, PairTile::kPerCu * PairTile::NW / 4) void linear_pair_kernel(
+    LinearGemmArgs x, Epilogue ex, LinearGemmArgs w, Epilogue ew, ColumnSums c, unsigned grid_x, unsigned grid_w, bool x_first) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   static_assert(64 * PairTile::NW == kSumThreads, "");
-  if (blockIdx.x < grid_w) linear_small_tile<true, true, PairTile, uint16_t>(w, ew, blockIdx.x, smem);
-  else if (blockIdx.x < grid_w + grid_x) linear_small_tile<false, false, PairTile, uint16_t>(x, ex, blockIdx.x - grid_w, smem);
-  else column_sums<uint16_t>(c, blockIdx.x - grid_w - grid_x, reinterpret_cast<float*>(smem));
+  const unsigned from_x = x_first ? 0 : grid_w, from_w = x_first ? grid_x : 0;
+  if (blockIdx.x >= grid_x + grid_w) column_sums<uint16_t>(c, blockIdx.x - grid_x - grid_w, reinterpret_cast<float*>(smem));
+  else if (blockIdx.x - from_x < grid_x) linear_small_tile<false, false, PairTile, uint16_t>(x, ex, blockIdx.x - from_x, smem);
+  else linear_small_tile<true, true, PairTile, uint16_t>(w, ew, blockIdx.x - from_w, smem);
 }
 
 template <typename G>
@@ -663,14 +665,15 @@ int launch_linear_bf16(const Product& p, void* ws, LinearSums& left, void* strea
   return launch<float>(p.a_tr, p.b_tr, a, sums, plan.shape, st);
 }
 
-// By the longer product and the mean of a CU's slices
+// By the longer product and the mean of a CU's slices; apart, they are another launch or two of 6.  (us, a backward
+// with an activation, together | apart: 1024 x 1024 x 1024 16 | 24, 4096 x 1024 x 1024 39 | 51, 2048 x 2048 x 2048 64 | 60.)
 bool linear_bf16_pair(int64_t M, int64_t N, int64_t K, int64_t Np) {
   constexpr int kTile = kShapes - 1;
   const double kx = (double)pair_plan(Np).slices_per_split, kw = (double)pair_plan(M).slices_per_split, longest = kx > kw ? kx : kw;
   const double tx = (double)tiles_of(kTile, M, K), tw = (double)tiles_of(kTile, K, N);
   const double cost = longest * kSliceUs[kTile][0] + (longest / 2 + (tx * kx + tw * kw) / 256) * kSliceUs[kTile][1] + kAroundUs[kTile][0] +
                       kAroundUs[kTile][1] * (tx + tw) / 256;
-  return cost < plan_of(false, false, M, K, Np).cost + plan_of(true, true, K, N, M).cost;
+  return cost < 6 + plan_of(false, false, M, K, Np).cost + plan_of(true, true, K, N, M).cost;
 }
 
 int launch_linear_bf16_pair(const Product& x, const Product& w, const ColumnSums& c, void* stream) {
@@ -678,7 +681,7 @@ int launch_linear_bf16_pair(const Product& x, const Product& w, const ColumnSums
   const unsigned grid_w = w.e.Y ? set_tiles<PairTile>(aw) : 0, grid_x = x.e.Y ? set_tiles<PairTile>(ax) : 0;
   if (hipError_t e0 = LdsLimit<&linear_pair_kernel, PairTile::kLds>::ensure(); e0 != hipSuccess) return (int)e0;
   hipLaunchKernelGGL(linear_pair_kernel, dim3(grid_w + grid_x + column_sum_blocks(c)), dim3(64 * PairTile::NW), PairTile::kLds,
-                     static_cast<hipStream_t>(stream), aw, w.e, ax, x.e, c, grid_w, grid_x);
+                     static_cast<hipStream_t>(stream), ax, x.e, aw, w.e, c, grid_x, grid_w, x.K > w.K);
   return (int)hipGetLastError();
 }
 
