@@ -470,11 +470,23 @@ int launch_skinny(const TunedGemmArgs& a, const E& e, hipStream_t stream) {
 // cost 3 us more).  Kernel above | this one: 1 x 1024 x 1024 4.9 | 4.0 us a product, 1 x 2048 x
 // 2048 7.3 | 6.3, 16 x 2048 x 2048 7.6 | 7.0; row form 1 x 2048 x 2048 0.7 less, 16 rows 0.2 more.
 // ---------------------------------------------------------------------------
-constexpr int kFewCols = 16, kFewTile = 1024;   // LDS of one product's transposed weights
+constexpr int kFewTile = 1024;   // LDS of one product's transposed weights
 // rows up to which it is the faster one, by the weights' form
-bool few_takes(bool b_tr, int64_t M) { return M <= (b_tr ? 16 : 8); }
-template <bool B_TR, typename E>
+bool few_takes(bool b_tr, int64_t M) { return M <= (b_tr ? kMostFewRows : 8); }
+// eight elements, those below `by` dropped and zeros following
+__device__ __forceinline__ u32x4 drop_low(u32x4 v, int by) {
+  uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+  if (by >= 8) lo = hi = 0;
+  else if (by >= 4) { lo = hi >> (16 * (by - 4)); hi = 0; }
+  else if (by > 0) { lo = lo >> (16 * by) | hi << (64 - 16 * by); hi >>= 16 * by; }
+  return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+// ANY (transposed weights, linear layer): K and N of 8 and more, rows wherever they lie.  16-byte loads need no more than
+// their elements' alignment; one that would pass an edge is moved back to end there, and what it then holds too much is
+// shifted out.  (Packing the operands first is a launch and two more passes over the weights.)
+template <bool B_TR, typename E, bool ANY = false>
 __global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_few_kernel(TunedGemmArgs a, E e) {
+  static_assert(!ANY || (B_TR && kLinear<E>), "");
   constexpr int NW = kSkinnyWaves, SL = kSkinnySlices;
   __shared__ __attribute__((aligned(16))) unsigned char smem[NW * SL * 2 * kFewTile];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -482,10 +494,11 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_few_kernel(TunedG
   const int64_t item = xcd_work_item(blockIdx.x, a.n_items);
   if (item >= a.n_items) return;
   const int64_t n0 = item * kFewCols;
-  const int KT = (int)(a.K / kSkinnyK);
+  const int KT = (int)(ANY ? (a.K + kSkinnyK - 1) / kSkinnyK : a.K / kSkinnyK);
   unsigned char* btile = smem + wave * (SL * 2 * kFewTile);
   const uint16_t* bsrc = B_TR ? a.B + (int64_t)(lane >> 1) * a.ldb + n0 + 8 * (lane & 1) : a.B + (n0 + i16) * a.ldb + 8 * gq;
   const uint16_t* asrc = a.A + i16 * a.lda + 8 * gq;
+  const int64_t col = n0 + 8 * (lane & 1), col_at = col + 8 <= a.N ? col : a.N - 8;   // (ANY)
   f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 
   for (int s0 = wave; s0 < KT; s0 += NW * SL) {
@@ -497,6 +510,13 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_few_kernel(TunedG
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int64_t k0 = (int64_t)sl * kSkinnyK + 32 * t;
+        if constexpr (ANY) {
+          const int64_t kw = k0 + (lane >> 1), kx = k0 + 8 * gq;
+          w[s][t] = *reinterpret_cast<const u32x4_any2*>(a.B + (kw < a.K ? kw : a.K - 1) * a.ldb + col_at);
+          x[s][t] = u32x4{0, 0, 0, 0};
+          if (i16 < a.M) x[s][t] = *reinterpret_cast<const u32x4_any2*>(a.A + i16 * a.lda + (kx + 8 <= a.K ? kx : a.K - 8));
+          continue;
+        }
         w[s][t] = *reinterpret_cast<const u32x4*>(B_TR ? bsrc + k0 * a.ldb : bsrc + k0);
         x[s][t] = u32x4{0, 0, 0, 0};
         if (i16 < a.M) x[s][t] = *reinterpret_cast<const u32x4*>(asrc + k0);
@@ -507,6 +527,14 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_few_kernel(TunedG
       if (s0 + NW * s >= KT) continue;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
+        if constexpr (ANY) {
+          const int64_t k0 = (int64_t)(s0 + NW * s) * kSkinnyK + 32 * t, kw = k0 + (lane >> 1), kx = k0 + 8 * gq;
+          if (n0 + kFewCols > a.N) w[s][t] = drop_low(w[s][t], (int)(col - col_at));
+          if (k0 + 32 > a.K) {
+            if (kw >= a.K) w[s][t] = u32x4{0, 0, 0, 0};
+            if (kx + 8 > a.K) x[s][t] = drop_low(x[s][t], kx < a.K ? (int)(kx + 8 - a.K) : 8);
+          }
+        }
         bf16x8 wf;
         if constexpr (B_TR) {   // (the wave's own slice: its reads follow its stores in the same queue)
           unsigned char* tile = btile + (2 * s + t) * kFewTile;
@@ -680,12 +708,17 @@ int launch_gemm_bf16(bool a_tr, bool b_tr, const void* A, int64_t lda, const voi
   return -1;   // transposed A with row-form B: no caller
 }
 
-int launch_linear_few_rows(const Product& p, void* stream) {
+int launch_linear_few_rows(const Product& p, bool any, void* stream) {
   TunedGemmArgs a = {};
   a.A = static_cast<const uint16_t*>(p.A);
   a.B = static_cast<const uint16_t*>(p.B);
   a.M = p.M; a.N = p.N; a.K = p.K; a.lda = p.lda; a.ldb = p.ldb;
-  return launch_few_rows(p.b_tr, a, p.e, static_cast<hipStream_t>(stream));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (!any) return launch_few_rows(p.b_tr, a, p.e, st);
+  a.n_items = (a.N + kFewCols - 1) / kFewCols;
+  hipLaunchKernelGGL((gemm_bf16_few_kernel<true, Epilogue, true>), dim3((unsigned)xcd_grid_size(a.n_items)), dim3(64 * kSkinnyWaves), 0, st, a,
+                     p.e);
+  return (int)hipGetLastError();
 }
 
 }  // namespace mhffn

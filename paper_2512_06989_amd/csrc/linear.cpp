@@ -26,6 +26,7 @@ struct Arena {
 // What has to be packed, and the padded sizes of what is
 struct Operands {
   bool x, w, dz;          // packed X [M][Kp], packed W [Kp][Np], dZ [M][Np] in the workspace
+  bool few;               // a few rows whose operands are read as they lie
   int64_t Kp, Np;
   Operands(const Linear& p, bool backward) {
     const bool bf16 = p.dtype == 1;
@@ -34,6 +35,12 @@ struct Operands {
     const bool y_fits = p.ldy <= kMostLd && (!bf16 || p.ldy % 8 == 0);
     x = p.ldx > kMostLd || (bf16 && ((backward ? p.K % 8 : p.K % 32) != 0 || p.ldx % 8 != 0));
     w = bf16 && (backward ? p.K % 8 != 0 || p.N % 32 != 0 : p.K % 32 != 0 || p.N % 8 != 0);
+    // Few rows and a width that nothing divides: instead of packing (us, as they lie | packed: 1 x 1001 x 515 5.4 | 9.5,
+    // 16 x 2048 x 5001 15 | 22, 1 x 2048 x 50257 61 | 140); a width that the tiles take, with one workgroup a CU at most
+    // (1 x 1000 x 1000 5.2 | 9.8, 1 x 4096 x 1000 6.3 | 12.0, 1 x 4128 x 4104 15.6 | 13.7)
+    few = !backward && bf16 && p.M <= kMostFewRows && p.K >= 8 && p.N >= 8 &&
+          (x || w || ((p.K % 64 != 0 || p.N % 32 != 0) && p.N <= 256 * kFewCols));
+    if (few) x = w = false;
     dz = backward && (p.act != 0 || p.drop.threshold != 0 || !y_fits || (bf16 && p.N % 32 != 0));
   }
 };
@@ -43,7 +50,7 @@ size_t partial_bytes(int dtype, bool a_tr, bool b_tr, int64_t M, int64_t N, int6
 }
 
 // Columns that the forward's product works on: with W packed its padding is there for the asking
-int64_t forward_columns(const Linear& p, const Operands& o) { return p.dtype != 1 ? p.N : o.w ? o.Np : up(p.N, 8); }
+int64_t forward_columns(const Linear& p, const Operands& o) { return p.dtype != 1 || o.few ? p.N : o.w ? o.Np : up(p.N, 8); }
 
 PackJob pack_x(const Linear& p, const Operands& o, const void* X, void* Xp) {
   return o.x ? PackJob{X, p.ldx, p.M, p.K, Xp, p.M, o.Kp} : PackJob{};
@@ -66,7 +73,7 @@ int forward(const Linear& p, const void* X, const void* W, const void* bias, con
   void* const Xp = o.x ? arena.take((size_t)p.M * o.Kp * elt(p.dtype)) : nullptr;
   void* const Wp = o.w ? arena.take((size_t)o.Kp * o.Np * 2) : nullptr;
   const int64_t K = bf16 && (o.x || o.w) ? o.Kp : p.K, N = forward_columns(p, o);
-  void* const P = arena.take(partial_bytes(p.dtype, false, true, p.M, N, K));
+  void* const P = o.few ? nullptr : arena.take(partial_bytes(p.dtype, false, true, p.M, N, K));
   if (bytes) {
     *bytes = arena.used;
     return 0;
@@ -80,6 +87,7 @@ int forward(const Linear& p, const void* X, const void* W, const void* bias, con
   e.act = p.act;
   e.drop = p.drop;
   const Product y = {false, true, o.x ? Xp : X, o.x ? o.Kp : p.ldx, o.w ? Wp : W, o.w ? o.Np : p.N, p.M, N, K, e};
+  if (o.few) return launch_linear_few_rows(y, true, stream);
   LinearSums left;
   rc = (bf16 ? launch_linear_bf16 : launch_linear_f32)(y, P, left, stream);
   return rc ? rc : launch_linear_sums(p.dtype, left, e, {}, {}, {}, stream);
@@ -139,6 +147,7 @@ std::string linear_plan(const Linear& p, bool back) {
   if (o.dz) s += "dZ ";
   if (p.dtype != 1) return s + (back ? linear_f32_pair_plan(p.M, p.N, p.K) : linear_f32_plan(p.M, p.N, p.K));
   const int64_t K8 = up(p.K, 8), N8 = up(p.N, 8);
+  if (o.few) return s + "few rows as they lie";
   if (!back) return s + linear_bf16_plan(false, true, p.M, forward_columns(p, o), o.x || o.w ? o.Kp : p.K);
   if (linear_bf16_pair(p.M, N8, K8, o.Np)) return s + linear_bf16_pair_plan();
   return s + "dX " + linear_bf16_plan(false, false, p.M, K8, o.Np) + "; dW " + linear_bf16_plan(true, true, K8, N8, p.M);

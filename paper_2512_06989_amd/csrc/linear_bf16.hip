@@ -655,7 +655,7 @@ size_t linear_bf16_workspace_bytes(bool a_tr, bool b_tr, int64_t M, int64_t N, i
 int launch_linear_bf16(const Product& p, void* ws, LinearSums& left, void* stream) {
   const Plan plan = plan_of(p.a_tr, p.b_tr, p.M, p.N, p.K);
   left = {};
-  if (plan.shape < 0) return launch_linear_few_rows(p, stream);
+  if (plan.shape < 0) return launch_linear_few_rows(p, false, stream);
   const LinearGemmArgs a = args_of(p, plan);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (plan.splits == 1) return launch<uint16_t>(p.a_tr, p.b_tr, a, p.e, plan.shape, st);

@@ -176,3 +176,31 @@ def test_a_captured_step_of_every_launch():
             want = step()
             torch.cuda.synchronize()
             assert all(torch.equal(a, c) for a, c in zip(got, want)), (dt, s, r)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 3, 16])
+@pytest.mark.parametrize("K", [8, 9, 31, 63, 64, 65, 100, 1001, 2063])
+@pytest.mark.parametrize("N", [8, 9, 15, 16, 17, 23, 40, 515, 4101])
+def test_a_few_rows_of_any_width(M, K, N):
+    """Both ends of both operands in the middle of NaN, the residual in place, the columns around Y left alone."""
+    X, W, b, R, _, _ = make(M, K, N, torch.bfloat16, 31, True, True)
+
+    def among_nan(t, before=16):
+        flat = torch.full((t.numel() + 64,), float("nan"), dtype=t.dtype, device="cuda")
+        inside = flat[before:before + t.numel()].view(t.shape)
+        inside.copy_(t)
+        return inside
+    wide = torch.full((M + 2, N + 5), 7.0, dtype=torch.bfloat16, device="cuda")
+    rows = wide.view(-1)[16:].as_strided((M, N), (N + 5, 1))
+    rows.copy_(R)
+    xs = torch.full((M * (K + 3) + 32,), float("nan"), dtype=torch.bfloat16, device="cuda")
+    Xs = xs[8:].as_strided((M, K), (K + 3, 1))
+    Xs.copy_(X)
+    rng = ref.rng_tensor(SEED, OFFSET, "cuda")
+    mhffn.linear_forward(Xs, among_nan(W), among_nan(b), rows, activation=mhffn.ACT_SILU, dropout=0.1, rng=rng, call=CALL, out={"Y": rows})
+    y, ey, _, _ = ref.forward(ref.f64(X), ref.f64(W), ref.f64(b), ref.f64(R), "silu", ref.multiplier(M, N, 0.1, SEED, OFFSET, CALL), torch.bfloat16)
+    ref.check(rows, y, ey, TOL["bf16"], "Y")
+    left = torch.ones_like(wide, dtype=torch.bool)
+    left.view(-1)[16:].as_strided((M, N), (N + 5, 1)).fill_(False)
+    assert torch.all(wide[left] == 7.0)
