@@ -273,8 +273,8 @@ int mhffn_module_backward(const mhffn_desc* desc, const void* X, const void* W_i
  *
  * n_rows, d_in and d_out take any size (rows from 0 to 2^28, widths from 1 to 2^20), row strides any
  * that is at least the width; rows that are not 16-byte aligned or lie more than 2^22 elements apart, and
- * widths that are no multiple of 32, cost copies of the operands in the workspace (fp32: only the rows far apart; the
- * forward of up to 16 rows in bf16: none).  Arithmetic is fp32 (bf16:
+ * widths that are no multiple of 32, cost copies of the operands in the workspace (fp32: only the rows far apart;
+ * bf16: such widths not in the forward of a few rows).  Arithmetic is fp32 (bf16:
  * products on the bf16 MFMA); Z and Y are rounded once to the storage type, and the
  * activation sees the unrounded Z.  The backward of an activation uses the rounded Z it is
  * given, and dZ is rounded to the storage type once more as an operand of its two products

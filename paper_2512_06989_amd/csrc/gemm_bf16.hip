@@ -472,7 +472,7 @@ int launch_skinny(const TunedGemmArgs& a, const E& e, hipStream_t stream) {
 // ---------------------------------------------------------------------------
 constexpr int kFewTile = 1024;   // LDS of one product's transposed weights
 // rows up to which it is the faster one, by the weights' form
-bool few_takes(bool b_tr, int64_t M) { return M <= (b_tr ? kMostFewRows : 8); }
+bool few_takes(bool b_tr, int64_t M) { return M <= (b_tr ? kFewRows : 8); }
 // eight elements, those below `by` dropped and zeros following
 __device__ __forceinline__ u32x4 drop_low(u32x4 v, int by) {
   uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
@@ -481,7 +481,7 @@ __device__ __forceinline__ u32x4 drop_low(u32x4 v, int by) {
   else if (by > 0) { lo = lo >> (16 * by) | hi << (64 - 16 * by); hi >>= 16 * by; }
   return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
-// ANY (transposed weights, linear layer): K and N of 8 and more, rows wherever they lie.  16-byte loads need no more than
+// ANY (transposed weights, linear layer): any rows, 16 a workgroup, K and N of 8 and more, wherever they lie.  16-byte loads need no more than
 // their elements' alignment; one that would pass an edge is moved back to end there, and what it then holds too much is
 // shifted out.  (Packing the operands first is a launch and two more passes over the weights.)
 template <bool B_TR, typename E, bool ANY = false>
@@ -493,7 +493,8 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_few_kernel(TunedG
   const int i16 = lane & 15, gq = lane >> 4;
   const int64_t item = xcd_work_item(blockIdx.x, a.n_items);
   if (item >= a.n_items) return;
-  const int64_t n0 = item * kFewCols;
+  const int64_t col_blocks = (a.N + kFewCols - 1) / kFewCols;
+  const int64_t n0 = (ANY ? item % col_blocks : item) * kFewCols, m0 = ANY ? item / col_blocks * kFewRows : 0;
   const int KT = (int)(ANY ? (a.K + kSkinnyK - 1) / kSkinnyK : a.K / kSkinnyK);
   unsigned char* btile = smem + wave * (SL * 2 * kFewTile);
   const uint16_t* bsrc = B_TR ? a.B + (int64_t)(lane >> 1) * a.ldb + n0 + 8 * (lane & 1) : a.B + (n0 + i16) * a.ldb + 8 * gq;
@@ -514,7 +515,7 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_few_kernel(TunedG
           const int64_t kw = k0 + (lane >> 1), kx = k0 + 8 * gq;
           w[s][t] = *reinterpret_cast<const u32x4_any2*>(a.B + (kw < a.K ? kw : a.K - 1) * a.ldb + col_at);
           x[s][t] = u32x4{0, 0, 0, 0};
-          if (i16 < a.M) x[s][t] = *reinterpret_cast<const u32x4_any2*>(a.A + i16 * a.lda + (kx + 8 <= a.K ? kx : a.K - 8));
+          if (m0 + i16 < a.M) x[s][t] = *reinterpret_cast<const u32x4_any2*>(a.A + (m0 + i16) * a.lda + (kx + 8 <= a.K ? kx : a.K - 8));
           continue;
         }
         w[s][t] = *reinterpret_cast<const u32x4*>(B_TR ? bsrc + k0 * a.ldb : bsrc + k0);
@@ -564,7 +565,7 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void gemm_bf16_few_kernel(TunedG
     const f32x4 lo4 = red[32 * q + row], hi4 = red[32 * q + 16 + row];
     float v[8] = {lo4[0], lo4[1], lo4[2], lo4[3], hi4[0], hi4[1], hi4[2], hi4[3]};
     EpilogueColumns<uint16_t> ec(e, n0 + 8 * q);
-    ec.finish(v, row, ec.residual(row, e), e, drop_key(e.drop));
+    ec.finish(v, m0 + row, ec.residual(m0 + row, e), e, drop_key(e.drop));
     return;
   }
   if (i16 < a.M)
@@ -715,7 +716,7 @@ int launch_linear_few_rows(const Product& p, bool any, void* stream) {
   a.M = p.M; a.N = p.N; a.K = p.K; a.lda = p.lda; a.ldb = p.ldb;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (!any) return launch_few_rows(p.b_tr, a, p.e, st);
-  a.n_items = (a.N + kFewCols - 1) / kFewCols;
+  a.n_items = (a.M + kFewRows - 1) / kFewRows * ((a.N + kFewCols - 1) / kFewCols);
   hipLaunchKernelGGL((gemm_bf16_few_kernel<true, Epilogue, true>), dim3((unsigned)xcd_grid_size(a.n_items)), dim3(64 * kSkinnyWaves), 0, st, a,
                      p.e);
   return (int)hipGetLastError();

@@ -9,7 +9,7 @@
 // v_mfma_f32_16x16x4_f32: lane (i16, gq) holds row i16 (column i16), k = gq.  Step s of 16 k takes k = 4 gq + s of both
 // operands, so that a lane of a row-form operand reads its four steps at once.  n is on the matrix row axis:
 // a lane ends up with four consecutive n of one row m, as in the bf16 product.  (4096^3: 124
-// TFLOP/s, a library product 154; 2000 x 2048 x 768, 64 x 64 tiles: 61 us, 128 x 128 71.)
+// TFLOP/s, a library product 154; 2000 x 2048 x 768, 64 x 64 tiles: 63 us, 128 x 128 71.)
 // LDS: row form [rows][32], 16-byte chunks permuted by (row / 2) % 8; transposed form [32 k][rows + 4] (the quarters of
 // a wave, four k apart, lie 16 banks apart): no bank conflicts in either.
 #include "epilogue.h"

@@ -35,11 +35,15 @@ struct Operands {
     const bool y_fits = p.ldy <= kMostLd && (!bf16 || p.ldy % 8 == 0);
     x = p.ldx > kMostLd || (bf16 && ((backward ? p.K % 8 : p.K % 32) != 0 || p.ldx % 8 != 0));
     w = bf16 && (backward ? p.K % 8 != 0 || p.N % 32 != 0 : p.K % 32 != 0 || p.N % 8 != 0);
-    // Few rows and a width that nothing divides: instead of packing (us, as they lie | packed: 1 x 1001 x 515 5.4 | 9.5,
-    // 16 x 2048 x 5001 15 | 22, 1 x 2048 x 50257 61 | 140); a width that the tiles take, with one workgroup a CU at most
-    // (1 x 1000 x 1000 5.2 | 9.8, 1 x 4096 x 1000 6.3 | 12.0, 1 x 4128 x 4104 15.6 | 13.7)
-    few = !backward && bf16 && p.M <= kMostFewRows && p.K >= 8 && p.N >= 8 &&
-          (x || w || ((p.K % 64 != 0 || p.N % 32 != 0) && p.N <= 256 * kFewCols));
+    // A width that nothing divides and few rows: the kernel for few rows reads the operands as they lie.  Instead of packing
+    // with up to 16 rows, or few rounds of one workgroup a CU; instead of tiles with one round.  (us, as they lie | packed:
+    // 1 x 1001 x 515 5.4 | 9.5, 16 x 2048 x 5001 15 | 22, 1 x 2048 x 50257 61 | 140, 64 x 1001 x 1001 6.5 | 10.2, 130 x 520 x
+    // 1000 7.6 | 10.4, 300 x 520 x 1000 11.2 | 10.5; | tiles: 1 x 4096 x 1000 6.3 | 12.0, 1 x 4128 x 4104 15.6 | 13.7.)  By sizes alone:
+    // the bits of a result do not depend on row strides.
+    const int64_t rounds = (up(p.M, kFewRows) / kFewRows * (up(p.N, kFewCols) / kFewCols) + 255) / 256;
+    few = !backward && bf16 && p.K >= 8 && p.N >= 8 &&
+          (p.K % 32 != 0 || p.N % 8 != 0 ? p.M <= kFewRows || rounds == 1 || rounds * (p.K + 300) <= 2500
+                                         : (p.K % 64 != 0 || p.N % 32 != 0) && rounds == 1);
     if (few) x = w = false;
     dz = backward && (p.act != 0 || p.drop.threshold != 0 || !y_fits || (bf16 && p.N % 32 != 0));
   }

@@ -158,9 +158,9 @@ struct Product {
 // bf16: N % 8 == 0 (e.N of the columns exist); row-form operands hold K % 32 == 0
 size_t linear_bf16_workspace_bytes(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K);
 int launch_linear_bf16(const Product& p, void* ws, LinearSums& left, void* stream);
-// Its kernels for a few rows (gemm_bf16.hip): N % 32 == 0, K % 64 == 0; `any`: transposed weights, up to 16 rows, K and
-// N from 8, rows wherever they lie
-constexpr int kMostFewRows = 16, kFewCols = 16;   // (columns a workgroup)
+// Its kernels for a few rows (gemm_bf16.hip): N % 32 == 0, K % 64 == 0; `any`: transposed weights, K and N from 8,
+// wherever they lie
+constexpr int kFewRows = 16, kFewCols = 16;   // of a workgroup
 int launch_linear_few_rows(const Product& p, bool any, void* stream);
 // fp32: any sizes, any strides
 size_t linear_f32_workspace_bytes(int64_t M, int64_t N, int64_t K);

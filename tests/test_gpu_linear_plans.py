@@ -179,7 +179,7 @@ def test_a_captured_step_of_every_launch():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("M", [1, 3, 16])
+@pytest.mark.parametrize("M", [1, 3, 16, 37])
 @pytest.mark.parametrize("K", [8, 9, 31, 63, 64, 65, 100, 1001, 2063])
 @pytest.mark.parametrize("N", [8, 9, 15, 16, 17, 23, 40, 515, 4101])
 def test_a_few_rows_of_any_width(M, K, N):
