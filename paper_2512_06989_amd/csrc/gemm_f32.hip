@@ -283,7 +283,7 @@ Epilogue epilogue_of(const Product& p, const F32Plan& plan, void* ws) {
   return e;
 }
 LinearSums left_of(const Product& p, const F32Plan& plan, void* ws) {
-  return plan.splits == 1 ? LinearSums{} : LinearSums{static_cast<float*>(ws), partial_ld(p.N), plan.splits};
+  return plan.splits == 1 ? LinearSums{} : LinearSums{static_cast<float*>(ws), p.M, partial_ld(p.N), plan.splits};
 }
 std::string text_of(const F32Plan& p) {
   return std::to_string(p.tile) + "x" + std::to_string(p.tile) + " splits=" + std::to_string(p.splits);

@@ -661,7 +661,7 @@ int launch_linear_bf16(const Product& p, void* ws, LinearSums& left, void* strea
   if (plan.splits == 1) return launch<uint16_t>(p.a_tr, p.b_tr, a, p.e, plan.shape, st);
   Epilogue sums = {};
   sums.Y = ws; sums.ldy = p.N; sums.M = p.M; sums.N = p.N;   // (N % 8 == 0)
-  left = {static_cast<float*>(ws), p.N, plan.splits};
+  left = {static_cast<float*>(ws), p.M, p.N, plan.splits};
   return launch<float>(p.a_tr, p.b_tr, a, sums, plan.shape, st);
 }
 

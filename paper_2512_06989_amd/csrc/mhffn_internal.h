@@ -135,9 +135,9 @@ int launch_linear_backward(const Linear& p, const void* X, const void* W, const 
 // Y = residual + D(X), X [M][N]; Y may be X or the residual
 int launch_dropout(int dtype, const void* X, int64_t ldx, const Epilogue& e, void* stream);
 // Kernels of pointwise.hip behind the host code of linear.cpp
-struct LinearSums {   // `splits` partial products P [splits][M][ldp] that an epilogue goes over (splits = 0: none)
+struct LinearSums {   // `splits` partial products P [splits][rows][ldp] that an epilogue goes over (splits = 0: none)
   const float* P;
-  int64_t ldp;
+  int64_t rows, ldp;   // of the product, padding among them: at least the epilogue's
   int splits;
 };
 struct ColumnSums {   // out[N] = the sum of partials [blocks][N] (blocks = 0: none)

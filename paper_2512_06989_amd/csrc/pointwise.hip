@@ -37,7 +37,7 @@ __device__ __forceinline__ void linear_sum(const LinearSums& s, const Epilogue& 
   load8(s.P + row * s.ldp + col, cols, v);
   for (int k = 1; k < s.splits; ++k) {
     float w[8];
-    load8(s.P + ((int64_t)k * e.M + row) * s.ldp + col, cols, w);
+    load8(s.P + ((int64_t)k * s.rows + row) * s.ldp + col, cols, w);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] += w[j];
   }
