@@ -600,9 +600,11 @@ int launch(bool a_tr, bool b_tr, const LinearGemmArgs& a, const Epilogue& e, int
 // Tile shape and split of the contraction.  Microseconds measured, with n tiles on the fullest CU: a slice of k takes
 // kSliceUs[0] + n kSliceUs[1] (what is shared by the workgroups of a CU hides a latency), what lies around the slices
 // kAroundUs[0] + n kAroundUs[1]; the sum over the splits is a launch of 4 and moves 5.7 MB a us.  The kernels for
-// few rows: up to 16 (weights in row form: 8) 16 columns a workgroup and 4.2 MB of weights a us at most, above 32 x 32.
-// (us: 24 x 2048 x 1024 few rows 5.7, the best split 64 x 64 9.1; 64 x 5632 x 2048 18.0 and 13.2;
-// 64 x 2048 x 5632, two of them on a CU, 18.5 and 12.9.)
+// few rows: up to 16 (weights in row form: 8) 16 columns a workgroup and 4.2 MB of weights a us at most, above 32 x 32 in one
+// round of one workgroup a CU (which also keeps their row blocks within a grid's second dimension, however narrow the layer).
+// (us, few rows | the best of tiles and splits: 24 x 2048 x 1024 5.7 | 9.1, 64 x 5632 x 2048 18.0 | 13.2, one round 8192 x 64 x 32
+// 4.1 | 4.0, 8192 x 1024 x 32 5.2 | 7.9, 2048 x 256 x 64 3.9 | 4.6, two 16384 x 64 x 32 5.9 | 4.2, 16384 x 1024 x 32 8.7 | 8.4, 8192 x
+// 512 x 64 7.6 | 5.8, 64 x 2048 x 5632 18.5 | 12.9, 128 rounds 1048576 x 64 x 64 581 | 65.)
 struct Plan { int shape, splits; int64_t slices_per_split; double cost; };   // shape -1: the kernels for few rows
 constexpr int kShapes = 5, kShapeM[kShapes] = {256, 256, 128, 64, 64}, kShapeN[kShapes] = {256, 128, 128, 128, 64};
 constexpr double kSliceUs[kShapes][2] = {{0, 0.72}, {0, 0.48}, {0, 0.277}, {0.045, 0.128}, {0.04, 0.08}};
@@ -622,10 +624,10 @@ Plan plan_of(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K) {
       if (best.cost == 0.0 || cost < best.cost) best = {sh, want, per, cost};
     }
   }
-  if (!a_tr && N % 32 == 0 && K % 64 == 0) {
-    const bool few = M <= (b_tr ? 16 : 8);
-    const int64_t wgs = few ? N / 16 : (M + 31) / 32 * (N / 32);
-    const double slices = (double)((wgs + 255) / 256) * (double)(K / 64) * (few ? 0.065 : wgs > 256 ? 0.22 : 0.13), weights = (double)K * N * 2 / 4.2e6;
+  const bool few = M <= (b_tr ? 16 : 8);
+  const int64_t wgs = few ? N / 16 : (M + 31) / 32 * (N / 32);
+  if (!a_tr && N % 32 == 0 && K % 64 == 0 && (few || wgs <= 256)) {
+    const double slices = (double)((wgs + 255) / 256) * (double)(K / 64) * (few ? 0.065 : 0.13), weights = (double)K * N * 2 / 4.2e6;
     const double cost = 3.3 + (few && weights > slices ? weights : slices);
     if (cost < best.cost) best = {-1, 1, KT, cost};
   }
