@@ -258,7 +258,7 @@ int mhffn_module_backward(const mhffn_desc* desc, const void* X, const void* W_i
  *   W [d_in][d_out] row-major, applied from the right; b [d_out]; both dense.
  *   Z [n_rows][d_out] dense.  Bias, residual R and Z are optional (NULL).
  *   act: none; relu max(z, 0); silu z / (1 + exp(-z)); gelu z Phi(z), Phi the normal
- *   distribution function.
+ *   distribution function.  At infinities act and its slope take their limits (act(-inf) = 0 but for none).
  *
  * D keeps an element and scales it by 65536 / (65536 - T), or makes it 0 whatever it held;
  * T = 65536 * dropout, rounded to the nearest whole number (dropout = 1: all are 0; T = 0:
