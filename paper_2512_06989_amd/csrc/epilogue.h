@@ -83,13 +83,13 @@ __device__ __forceinline__ NormalTail normal_tail(float z) {
   return n;
 }
 // NaN stays NaN in each, infinities give the limits: a factor z next to one that has vanished is held to a finite value (128
-// for silu, 30 for gelu; past them the other factor is 0 or 1).  Results of type T: fp32 takes the library's erf (its products are sixteen
-// times as long), bf16 the tail above: 40 instructions an element against 16.
+// for silu, 30 for gelu; past them the other factor is 0 or 1).  Results of type T: fp32 takes the library's erfc (its products are
+// sixteen times as long; 1 + erf would cancel for negative z: a digit is left at -5; a forward of 2000 x 768 x 2048 67.0 us, with erf 65.0), bf16 the tail above.
 template <int ACT, typename T>
 __device__ __forceinline__ float activate(float z) {
   if constexpr (ACT == 1) return z < 0.f ? 0.f : z;
   else if constexpr (ACT == 2) return fmaxf(z, -128.f) * sigmoid_fast(z);
-  else if constexpr (ACT == 3 && sizeof(T) == 4) return 0.5f * fmaxf(z, -30.f) * (1.f + erff(z * 0.70710678118654752f));
+  else if constexpr (ACT == 3 && sizeof(T) == 4) return 0.5f * fmaxf(z, -30.f) * erfcf(-0.70710678118654752f * z);
   else if constexpr (ACT == 3) {
     const NormalTail n = normal_tail(z);
     return (z < 0.f ? 0.f : z) - n.a * n.q;   // z Phi(z)
@@ -103,7 +103,7 @@ __device__ __forceinline__ float slope(float z) {
     const float s = sigmoid_fast(z);
     return s + fminf(fmaxf(z, -128.f), 128.f) * s * (1.f - s);
   } else if constexpr (ACT == 3 && sizeof(T) == 4) {
-    return 0.5f * (1.f + erff(z * 0.70710678118654752f)) +
+    return 0.5f * erfcf(-0.70710678118654752f * z) +
            fminf(fmaxf(z, -30.f), 30.f) * (0.39894228040143268f * __builtin_amdgcn_exp2f(-0.5f * MHFFN_LOG2E * z * z));
   } else if constexpr (ACT == 3) {
     const NormalTail n = normal_tail(z);
