@@ -309,7 +309,7 @@ int mhffn_linear_forward(const mhffn_linear_desc* desc, const void* X, const voi
                          const void* bias, const void* residual, const void* rng, void* Y,
                          void* Z, void* workspace, size_t workspace_bytes, void* hip_stream);
 
-/* dZ = D(dY) act'(Z);  dX = dZ W^T;  dW = X^T dZ;  dbias = the column sums of dZ.  Any
+/* dZ = D(dY act'(Z));  dX = dZ W^T;  dW = X^T dZ;  dbias = the column sums of dZ.  Any
  * gradient may be NULL => not computed.  Z is read unless the activation is none (relu'(0) = 0).  The
  * gradient of the residual is dY itself.  No gradient may overlap an input. */
 int mhffn_linear_backward(const mhffn_linear_desc* desc, const void* X, const void* W,

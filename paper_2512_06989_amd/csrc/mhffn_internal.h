@@ -182,7 +182,7 @@ struct PackJob {
   int64_t rows_to, cols_to;
 };
 int launch_pack(int dtype, const PackJob& a, const PackJob& b, void* stream);
-// dZ = D(dY) act'(Z) into dZ [M][ldz] (zero past column N; may be NULL), its column sums into
+// dZ = D(dY act'(Z)) into dZ [M][ldz] (zero past column N; may be NULL), its column sums into
 // dbias (may be NULL) by way of `partials` (linear_column_blocks(M, N) x N floats)
 struct LinearDz {
   const void* dY;

@@ -111,12 +111,12 @@ __global__ __launch_bounds__(kThreads) void linear_dz_kernel(LinearDz a, DzGrid 
       float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
       if (cols > 0) {
         load8(static_cast<const T*>(a.dY) + row * a.ldy + col, cols, v);
-        drop8(v, (uint64_t)row * per_row + piece, a.drop, key);
         if (a.act) {
           float z[8];
           load8(static_cast<const T*>(a.Z) + row * a.N + col, cols, z);
           slope8<T>(v, z, a.act);
         }
+        drop8(v, (uint64_t)row * per_row + piece, a.drop, key);   // (last: a dropped element may hold anything in Z and dY)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] += v[j];
       }
