@@ -277,8 +277,8 @@ int mhffn_module_backward(const mhffn_desc* desc, const void* X, const void* W_i
  * bf16: such widths not in the forward of a few rows).  Arithmetic is fp32 (bf16:
  * products on the bf16 MFMA); Z and Y are rounded once to the storage type, and the
  * activation sees the unrounded Z.  The backward of an activation uses the rounded Z it is
- * given, and dZ is rounded to the storage type once more as an operand of its two products
- * (not in db).  Sums are added in a fixed order: results are bit-identical from run to run. */
+ * given, and dZ, before the dropout's scale, is rounded to the storage type once more as an operand of its
+ * two products (not in db): without an activation and with relu that loses nothing.  Sums are added in a fixed order: results are bit-identical from run to run. */
 typedef enum {
   MHFFN_ACT_NONE = 0,
   MHFFN_ACT_RELU = 1,

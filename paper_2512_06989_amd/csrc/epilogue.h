@@ -48,7 +48,7 @@ __device__ __forceinline__ u32x4 philox4x32_10(uint64_t piece, const DropKey& ke
 }
 
 // A dropped element is 0 whatever it held, infinities and NaN among it.
-__device__ __forceinline__ void drop8(float (&v)[8], uint64_t piece, const Dropout& d, const DropKey& key) {
+__device__ __forceinline__ void drop8(float (&v)[8], uint64_t piece, const Dropout& d, const DropKey& key, float scale) {
   if (d.threshold == 0) return;
   if (d.threshold > 65535) {
 #pragma unroll
@@ -59,7 +59,7 @@ __device__ __forceinline__ void drop8(float (&v)[8], uint64_t piece, const Dropo
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const uint32_t half = j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xFFFFu;
-    v[j] = half >= d.threshold ? v[j] * d.scale : 0.f;
+    v[j] = half >= d.threshold ? v[j] * scale : 0.f;
   }
 }
 
@@ -236,13 +236,17 @@ struct EpilogueColumns {
   // v: the product's eight sums
   __device__ __forceinline__ void finish(float (&v)[8], int64_t row, const Raw8<T>& res, const Epilogue& e, const DropKey& key) const {
     if (row >= e.M || cols <= 0) return;
+    if (e.scale != 1.f) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] *= e.scale;
+    }
     if (e.bias) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += bias[j];
     }
     if (e.Z) store8(static_cast<T*>(e.Z) + row * e.ldz + col, cols, v);
     activate8<T>(v, e.act);
-    drop8(v, (uint64_t)row * (uint64_t)((e.N + 7) >> 3) + (uint64_t)(col >> 3), e.drop, key);
+    drop8(v, (uint64_t)row * (uint64_t)((e.N + 7) >> 3) + (uint64_t)(col >> 3), e.drop, key, e.drop.scale);
     if (e.residual) {
       float r[8];
       unpack8(res, r);

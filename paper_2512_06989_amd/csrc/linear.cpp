@@ -63,9 +63,10 @@ PackJob pack_w(const Linear& p, const Operands& o, const void* W, void* Wp) {
   return o.w ? PackJob{W, p.N, p.K, p.N, Wp, o.Kp, o.Np} : PackJob{};
 }
 
-Epilogue plain(void* Y, int64_t ldy, int64_t M, int64_t N) {
+Epilogue plain(void* Y, int64_t ldy, int64_t M, int64_t N, float scale = 1.f) {
   Epilogue e = {};
   e.Y = Y; e.ldy = ldy; e.M = M; e.N = N;
+  e.scale = scale;
   return e;
 }
 
@@ -128,8 +129,8 @@ int backward(const Linear& p, const void* X, const void* W, const void* Z, const
   const int64_t ldg = o.dz ? ldz : p.ldy;
   rc = launch_pack(p.dtype, dW ? pack_x(p, o, X, Xp) : PackJob{}, dX ? pack_w(p, o, W, Wp) : PackJob{}, stream);
   if (rc) return rc;
-  const Product x = {false, false, G, ldg, o.w ? Wp : W, o.w ? o.Np : p.N, p.M, K8, o.Np, plain(dX, p.ldx, p.M, p.K)};
-  const Product w = {true, true, o.x ? Xp : X, o.x ? o.Kp : p.ldx, G, ldg, K8, N8, p.M, plain(dW, p.N, p.K, p.N)};
+  const Product x = {false, false, G, ldg, o.w ? Wp : W, o.w ? o.Np : p.N, p.M, K8, o.Np, plain(dX, p.ldx, p.M, p.K, p.drop.scale)};
+  const Product w = {true, true, o.x ? Xp : X, o.x ? o.Kp : p.ldx, G, ldg, K8, N8, p.M, plain(dW, p.N, p.K, p.N, p.drop.scale)};
   LinearSums left_x = {}, left_w = {};
   if (pair && (dX || dW)) {   // (one alone too: its bits do not depend on what else is asked for)
     if (bf16) return launch_linear_bf16_pair(x, w, columns, stream);

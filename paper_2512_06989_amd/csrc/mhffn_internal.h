@@ -119,6 +119,7 @@ struct Epilogue {
   int64_t ldr, ldz, ldy, M, N;
   int act;               // mhffn_activation
   Dropout drop;
+  float scale = 1.f;     // of the product (a backward's dropout)
 };
 struct Linear {
   int64_t M;             // rows
@@ -182,7 +183,7 @@ struct PackJob {
   int64_t rows_to, cols_to;
 };
 int launch_pack(int dtype, const PackJob& a, const PackJob& b, void* stream);
-// dZ = D(dY act'(Z)) into dZ [M][ldz] (zero past column N; may be NULL), its column sums into
+// dZ = D(dY act'(Z)) without D's scale into dZ [M][ldz] (zero past column N; may be NULL), its column sums, scaled, into
 // dbias (may be NULL) by way of `partials` (linear_column_blocks(M, N) x N floats)
 struct LinearDz {
   const void* dY;

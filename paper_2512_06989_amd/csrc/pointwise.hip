@@ -86,6 +86,10 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(PackJob a, Pieces pa, Pa
   }
 }
 
+// dZ is rounded to the storage type, as the operand of two products (in bf16: the MFMA's operand; the columns' sums take it
+// unrounded).  The dropout's scale is left to the products' sums: without an activation, or with relu, dZ is dY or 0 and
+// the rounding costs nothing; with a slope it is a second rounding of the gradients (bf16, GELU: 2.35e-3 of their norm in place of 1.66e-3;
+// products of both halves of a split dZ would cost twice the matrix time).
 // Lane t of a workgroup takes piece column t % lanes of rows t / lanes, + rows_at_once, ..: the
 // workgroup's share of dZ, and the sums of its eight columns per lane, which meet in LDS in row
 // order and go out as one partial sum per column and row block.
@@ -116,7 +120,7 @@ __global__ __launch_bounds__(kThreads) void linear_dz_kernel(LinearDz a, DzGrid 
           load8(static_cast<const T*>(a.Z) + row * a.N + col, cols, z);
           slope8<T>(v, z, a.act);
         }
-        drop8(v, (uint64_t)row * per_row + piece, a.drop, key);   // (last: a dropped element may hold anything in Z and dY)
+        drop8(v, (uint64_t)row * per_row + piece, a.drop, key, 1.f);   // (last: a dropped element may hold anything in Z and dY)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] += v[j];
       }
@@ -131,7 +135,7 @@ __global__ __launch_bounds__(kThreads) void linear_dz_kernel(LinearDz a, DzGrid 
     float sum = 0.f;
     for (int k = 0; k < at_once; ++k) sum += sums[k * 8 * lanes + t];
     const int64_t c = (int64_t)blockIdx.x * 8 * lanes + t;
-    if (c < a.N) a.partials[(int64_t)blockIdx.y * a.N + c] = sum;
+    if (c < a.N) a.partials[(int64_t)blockIdx.y * a.N + c] = sum * a.drop.scale;
   }
 }
 
