@@ -111,7 +111,13 @@ struct OnStream {
   OnStream& operator=(const OnStream&) = delete;
 };
 
-// The caller's workspace, or a fresh one of the size the library asks for.  It is given back when
+// The caller's workspace: dense memory of the tensors' device (its bytes are counted by its elements)
+at::Tensor workspace_of(PyObject* given, const at::Tensor& x) {
+  const at::Tensor t = tensor(given);
+  require(t.device() == x.device() && t.is_contiguous());
+  return t;
+}
+// That, or a fresh one of the size the library asks for.  It is given back when
 // the call returns, so it has to belong to the stream the kernels run on: only what follows
 // them there may get its memory.
 struct Workspace {
@@ -119,7 +125,7 @@ struct Workspace {
   size_t bytes = 0;
   Workspace(const Problem& p, int op, PyObject* given, PyObject* stream) {
     if (given != Py_None) {
-      t = tensor(given);
+      t = workspace_of(given, p.x);
     } else if (const size_t need = mhffn_workspace_bytes(&p.d, op)) {
       std::optional<OnStream> guard;
       if (stream != Py_None && p.x.is_cuda()) guard.emplace(stream_of(stream), p.x);
@@ -319,7 +325,7 @@ int32_t dtype_code(const at::Tensor& x) {
   return x.scalar_type() == at::kBFloat16 ? MHFFN_BF16 : MHFFN_F32;
 }
 at::Tensor scratch(size_t need, PyObject* given, PyObject* stream, const at::Tensor& x) {
-  if (given != Py_None) return tensor(given);
+  if (given != Py_None) return workspace_of(given, x);
   if (need == 0) return at::Tensor();
   std::optional<OnStream> guard;
   if (stream != Py_None && x.is_cuda()) guard.emplace(stream_of(stream), x);

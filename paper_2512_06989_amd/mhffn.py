@@ -235,10 +235,18 @@ def workspace_bytes(desc, op):
     return int(load().mhffn_workspace_bytes(ctypes.byref(desc), int(op)))
 
 
-def _workspace(desc, op, device, workspace):
+def _check_workspace(workspace, X):
+    """A caller's workspace: dense memory on X's device (its bytes are counted by its elements)."""
+    if workspace is not None:
+        _require(workspace.device == X.device, "workspace is on %s, expected %s" % (workspace.device, X.device))
+        _require(workspace.is_contiguous(), "workspace must be contiguous")
+
+
+def _workspace(desc, op, X, workspace):
+    _check_workspace(workspace, X)
     need = workspace_bytes(desc, op)
     if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        workspace = torch.empty(need, dtype=torch.uint8, device=X.device)
     have = 0 if workspace is None else workspace.numel() * workspace.element_size()
     return workspace, have
 
@@ -252,6 +260,7 @@ def forward(X, W_gate, W_up, W_down, route, eps=1e-6, route_mode=ROUTE_PARAMS, o
     if r is None:
         _check_params(X, W_gate, W_up, W_down, route, route_mode)
         make_desc(X, W_gate, route_mode, eps, out)
+        _check_workspace(workspace, X)
         raise ValueError("forward: invalid arguments")
     return _result(r, "mhffn_forward")
 
@@ -301,6 +310,7 @@ def backward(X, W_gate, W_up, W_down, route, dY, eps=1e-6, route_mode=ROUTE_PARA
         _check_params(X, W_gate, W_up, W_down, route, route_mode)
         d = make_desc(X, W_gate, route_mode, eps, dY)
         _grad_outputs(X, W_gate, W_up, W_down, route, want, out, d.ld_x)
+        _check_workspace(workspace, X)
         raise ValueError("backward: invalid arguments")
     return _result(r, "mhffn_backward")
 
@@ -325,7 +335,7 @@ def reference_unfused(X, W_gate, W_up, W_down, route, eps=1e-6, route_mode=ROUTE
                               {k: v for k, v in out.items() if k != "Y"}, d.ld_x)
         out.update(grads)
     op = OP_UNFUSED_FORWARD if dY is None else OP_UNFUSED_BACKWARD
-    workspace, have = _workspace(d, op, X.device, workspace)
+    workspace, have = _workspace(d, op, X, workspace)
     rc = load().mhffn_reference_unfused(
         ctypes.byref(d), _p(X), _p(W_gate), _p(W_up), _p(W_down), _p(route), _p(Y), _p(dY),
         _p(out.get("dX")), _p(out.get("dW_gate")), _p(out.get("dW_up")), _p(out.get("dW_down")),
@@ -400,6 +410,7 @@ def linear_forward(X, W, bias=None, residual=None, activation=ACT_NONE, dropout=
         if out.get("Z") is not None:
             _dense("Z", out["Z"], shape, X.dtype, X.device)
         _check_dropout(dropout, rng, call, X.device)
+        _check_workspace(workspace, X)
         _check_device(X)
         raise ValueError("linear_forward: invalid arguments")
     return _result(r, "mhffn_linear_forward")
@@ -432,6 +443,7 @@ def linear_backward(X, W, dY, Z=None, activation=ACT_NONE, dropout=0.0, rng=None
             if out.get(k) is not None:
                 _dense(k, out[k], t, X.dtype, X.device)
         _check_dropout(dropout, rng, call, X.device)
+        _check_workspace(workspace, X)
         _check_device(X)
         raise ValueError("linear_backward: invalid arguments")
     r = _result(r, "mhffn_linear_backward")
@@ -480,6 +492,7 @@ def module_forward(X, W_in, W_gate, W_up, W_down, W_r, W_out, eps=1e-6, out=None
             if k in out:
                 _dense(k, out[k], (N, dm), X.dtype, X.device)
         make_desc(X, W_gate, ROUTE_PARAMS, eps, out.get("O"))
+        _check_workspace(workspace, X)
         raise ValueError("module_forward: invalid arguments")
     return _result(r, "mhffn_module_forward")
 
@@ -512,6 +525,7 @@ def module_backward(X, W_in, W_gate, W_up, W_down, W_r, W_out, Q, S, dO, eps=1e-
         for k, ref in like.items():
             if out.get(k) is not None:
                 _dense(k, out[k], ref.shape, ref.dtype, ref.device)
+        _check_workspace(workspace, X)
         raise ValueError("module_backward: invalid arguments")
     r = _result(r, "mhffn_module_backward")
     return {k: r[k] for k in want}
