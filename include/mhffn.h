@@ -268,8 +268,9 @@ int mhffn_module_backward(const mhffn_desc* desc, const void* X, const void* W_i
  * (i * ceil(n / 8) + j / 8, offset + call), 64 bits each, low words first.  `rng` points to
  * { seed, offset } in DEVICE memory, 8-byte aligned, read when the kernels run: a program that replays a
  * captured graph advances the offset between replays, and the backward of a pass is given
- * what its forward was given.  `call` tells the dropouts of one step apart.  With T = 0 rng
- * may be NULL.
+ * what its forward was given.  `call` tells the dropouts of one step apart: it is added to the
+ * offset, so a step whose calls are 0 .. n - 1 advances the offset by at least n (advanced by less, a
+ * call draws the mask that another one had in the step before).  With T = 0 rng may be NULL.
  *
  * n_rows, d_in and d_out take any size (rows from 0 to 2^28, widths from 1 to 2^20), row strides any
  * that is at least the width; rows that are not 16-byte aligned or lie more than 2^22 elements apart, and

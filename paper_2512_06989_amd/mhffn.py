@@ -457,7 +457,8 @@ def dropout(X, p, rng, call=0, residual=None, out=None, stream=None):
     Which elements stay follows from `rng`, an int64 tensor (seed, offset) on X's device, the number
     `call` and the element's place alone (Philox4x32-10, see mhffn.h) and is never stored: the
     backward is the same call on dY, without the residual.  The kernels read rng when they run, so a
-    captured graph draws new numbers once the offset has been advanced."""
+    captured graph draws new numbers once the offset has been advanced: by at least the number of
+    different `call`s of a step, since the mask belongs to offset + call."""
     r = (_host or _load_host()).dropout(X, p, rng, call, residual, out, _raw(stream))
     if r is None:
         _require(X.dim() == 2, "X must be [N, n], got %s" % (tuple(X.shape),))
