@@ -103,7 +103,7 @@ int check_dropout(float p, const void* rng, uint64_t call, bool reads, mhffn::Dr
   return (reinterpret_cast<uintptr_t>(rng) & 7u) ? MHFFN_ERR_ALIGN : MHFFN_OK;
 }
 
-// (linear: a launch holds fewer than 2^32 threads, and the narrowest tiles take four a row)
+// (linear: a launch holds fewer than 2^32 threads, and the narrowest layers take four a row)
 constexpr int64_t kMostRows = (int64_t)1 << 40, kMostLinearRows = 1 << 28, kMostWidth = 1 << 20;
 
 int check_linear(const mhffn_linear_desc* d, const void* rng, mhffn::Linear* p) {

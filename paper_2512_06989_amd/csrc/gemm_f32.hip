@@ -216,7 +216,7 @@ F32Plan plan_f32(int64_t M, int64_t N, int64_t K) {
     const int64_t tiles = tiles_of(M, N, tile);
     for (int want = 1; want <= kMostSplits; ++want) {
       const int64_t per = share_of(K, want);
-      if (!per) continue;
+      if (!per || !launch_holds(tiles * want, kFThreads)) continue;
       const double n = (double)((tiles * want + 255) / 256);
       const double cost = (double)(per / kFK) * (kAlone[t] + kSlice[t] * n) + 2 + n + sum_cost(M, N, want);
       if (best.cost == 0.0 || cost < best.cost) best = {tile, want, per, cost};
@@ -235,7 +235,7 @@ F32Pair plan_f32_pair(int64_t M, int64_t N, int64_t K) {   // the layer's sizes
     const int64_t px = share_of(N, sx);
     for (int sw = 1; px && sw <= kMostSplits; ++sw) {
       const int64_t pw = share_of(M, sw);
-      if (!pw) continue;
+      if (!pw || !launch_holds(tx * sx + tw * sw, kFThreads)) continue;
       const double longest = (double)((px > pw ? px : pw) / kFK), mean = (double)(tx * sx * px + tw * sw * pw) / kFK / 256;
       const double cost = longest * kAlone[1] + (0.5 * longest + mean) * kSlice[1] + 2 + (double)(tx * sx + tw * sw) / 256 +
                           sum_cost(M, K, sx) + sum_cost(K, N, sw);

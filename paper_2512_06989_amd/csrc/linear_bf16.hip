@@ -607,6 +607,7 @@ int launch(bool a_tr, bool b_tr, const LinearGemmArgs& a, const Epilogue& e, int
 // 512 x 64 7.6 | 5.8, 64 x 2048 x 5632 18.5 | 12.9, 128 rounds 1048576 x 64 x 64 581 | 65.)
 struct Plan { int shape, splits; int64_t slices_per_split; double cost; };   // shape -1: the kernels for few rows
 constexpr int kShapes = 5, kShapeM[kShapes] = {256, 256, 128, 64, 64}, kShapeN[kShapes] = {256, 128, 128, 128, 64};
+constexpr int kShapeThreads[kShapes] = {512, 512, 512, 256, 256};
 constexpr double kSliceUs[kShapes][2] = {{0, 0.72}, {0, 0.48}, {0, 0.277}, {0.045, 0.128}, {0.04, 0.08}};
 constexpr double kAroundUs[kShapes][2] = {{1, 12}, {3, 6}, {2, 4}, {3.5, 1.6}, {3.3, 0.73}};
 int64_t tiles_of(int sh, int64_t M, int64_t N) { return ((M + kShapeM[sh] - 1) / kShapeM[sh]) * ((N + kShapeN[sh] - 1) / kShapeN[sh]); }
@@ -618,6 +619,7 @@ Plan plan_of(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K) {
     for (int want = 1; want <= 16; ++want) {
       const int64_t per = (KT + want - 1) / want;
       if (want > 1 && (per < 8 || (KT + per - 1) / per != want)) continue;   // at least eight slices per workgroup
+      if (!launch_holds(tiles * want, kShapeThreads[sh])) continue;
       const double n = (double)((tiles * want + 255) / 256);
       double cost = (double)per * (kSliceUs[sh][0] + kSliceUs[sh][1] * n) + kAroundUs[sh][0] + kAroundUs[sh][1] * n;
       if (want > 1) cost += 4 + (double)want * M * N * 4 / 5.7e6;
@@ -673,6 +675,7 @@ bool linear_bf16_pair(int64_t M, int64_t N, int64_t K, int64_t Np) {
   constexpr int kTile = kShapes - 1;
   const double kx = (double)pair_plan(Np).slices_per_split, kw = (double)pair_plan(M).slices_per_split, longest = kx > kw ? kx : kw;
   const double tx = (double)tiles_of(kTile, M, K), tw = (double)tiles_of(kTile, K, N);
+  if (!launch_holds(tiles_of(kTile, M, K) + tiles_of(kTile, K, N) + N, kShapeThreads[kTile])) return false;   // (N: more than the columns' workgroups)
   const double cost = longest * kSliceUs[kTile][0] + (longest / 2 + (tx * kx + tw * kw) / 256) * kSliceUs[kTile][1] + kAroundUs[kTile][0] +
                       kAroundUs[kTile][1] * (tx + tw) / 256;
   return cost < 6 + plan_of(false, false, M, K, Np).cost + plan_of(true, true, K, N, M).cost;

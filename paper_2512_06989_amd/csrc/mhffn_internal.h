@@ -156,6 +156,8 @@ struct Product {
   int64_t ldb, M, N, K;
   Epilogue e;
 };
+// A launch holds fewer than 2^32 threads: tall outputs in small tiles may have more (2^28 x 320 in 64 x 64: 5.4e9)
+inline bool launch_holds(int64_t workgroups, int threads) { return (workgroups + 16) * threads < (int64_t)1 << 32; }   // (16: grids of whole eights)
 // bf16: N % 8 == 0 (e.N of the columns exist); row-form operands hold K % 32 == 0
 size_t linear_bf16_workspace_bytes(bool a_tr, bool b_tr, int64_t M, int64_t N, int64_t K);
 int launch_linear_bf16(const Product& p, void* ws, LinearSums& left, void* stream);
